@@ -287,6 +287,96 @@ ogq_status ogq_bucket_decode_sum(const uint32_t *const *d_packed_k, const float 
                                  ogq_stream_t stream);
 
 /*
+ * Activation checkpoints in 8 bits, and the training operators that write and read them.  Data-parallel training keeps two
+ * things besides its weights: the gradient, which the calls above compress for the wire, and the activations that a layer's
+ * backward pass needs, which these calls keep in 8.25 bits a value.
+ *
+ * Types: `dtype` is the type of the activations and of their gradients, one of ogq_dtype.  Parameters, statistics and the
+ * gradients of parameters are fp32 (the gradient of a weight can so be written straight into the gradient bucket).
+ * Arithmetic is fp32 whatever the type; a result is rounded once, to nearest.
+ *
+ * Format of a matrix [rows, cols].  d_codes: int8 [rows, cols], contiguous.  d_scales: uint8 [rows, ogq_act8_groups(cols)],
+ * contiguous; byte j of a row belongs to the row's columns 32 j ... 32 j + 31 (the last group may be shorter).
+ *   A byte b in 1 ... 254 stands for the unit 2^(b-127), 255 for NaN, 0 for 0; the value of an element is its code times the
+ *   unit of its group, which has at most 7 significant bits and is exact in bf16 and fp32.
+ *   The encoder takes e = the smallest integer with max|x| <= 127 * 2^e over the group, at least -120 and at most 121, and
+ *   b = e + 127.  OGQ_ROUND_NEAREST: code = x / 2^e rounded to the nearest integer, ties to even.  OGQ_ROUND_RANDOM: unbiased, as
+ *   the gradient quantizer: t = x / 2^e, code = floor(t), plus one if (float)u < (t - floor(t)) * 2^24, each operation in fp32; u is
+ *   the top 24 bits of word (i mod 4) of Philox4x32-10 with key (seed low, seed high) and counter (i/4 low, i/4 high, which,
+ *   stream_id), i = row * cols + column, `which` 0 (1 for the gate's input d_up).  Codes lie in -127 ... 127.
+ *   A group with a NaN or an infinity gets byte 255 and codes 0, so that all of it reads as NaN.
+ *
+ * Matrices of activations have a row stride ld (in elements, at least cols); columns beyond cols are not touched.  Pointers need the
+ * alignment of their type only; calls with pointers on 16-byte boundaries (codes: 8), and cols and strides that are multiples of 8, are faster.
+ * Outputs must not overlap inputs, except that d_y may be d_x and d_dx may be d_dy (same stride).  rows * ogq_act8_groups(cols)
+ * must be below 2^31 (OGQ_ERR_UNSUPPORTED).  rows = 0 or cols = 0 is allowed and writes nothing.
+ *
+ *   ogq_act8_encode / ogq_act8_decode: a matrix into this form and back.  A value beyond the range of fp16 decodes to an infinity there.
+ *   ogq_act8_forward: y = f(x), or f(x) * up when d_up is given; keeps x (and up) in 8 bits.
+ *   ogq_act8_backward: dx = dy f'(x^) [up^], dup = dy f(x^), from the kept x^ [and up^].  d_dup, d_up_codes and d_up_scales are all
+ *     given or all NULL.
+ * f is one of ogq_activation: the identity, ReLU (slope 0 at 0), x / (1 + exp(-x)), x Phi(x) with Phi the normal distribution function.
+ */
+typedef enum { OGQ_F32 = 0, OGQ_F16 = 1, OGQ_BF16 = 2 } ogq_dtype;
+typedef enum { OGQ_ACT_NONE = 0, OGQ_ACT_RELU = 1, OGQ_ACT_SILU = 2, OGQ_ACT_GELU = 3 } ogq_activation;
+typedef enum { OGQ_ROUND_NEAREST = 0, OGQ_ROUND_RANDOM = 1 } ogq_rounding;
+
+int64_t ogq_act8_groups(int64_t cols); /* ceil(cols / 32); -1 if cols < 0 */
+ogq_status ogq_act8_encode(const void *d_x, int64_t ld_x, int64_t rows, int64_t cols, int dtype, int rounding,
+                           uint64_t seed, uint32_t stream_id, int8_t *d_codes, uint8_t *d_scales,
+                           ogq_stream_t stream);
+ogq_status ogq_act8_decode(const int8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, int dtype,
+                           void *d_x, int64_t ld_x, ogq_stream_t stream);
+ogq_status ogq_act8_forward(const void *d_x, int64_t ld_x, const void *d_up, int64_t ld_up, int64_t rows,
+                            int64_t cols, int dtype, int act, int rounding, uint64_t seed, uint32_t stream_id,
+                            void *d_y, int64_t ld_y, int8_t *d_codes, uint8_t *d_scales, int8_t *d_up_codes,
+                            uint8_t *d_up_scales, ogq_stream_t stream);
+ogq_status ogq_act8_backward(const void *d_dy, int64_t ld_dy, const int8_t *d_codes, const uint8_t *d_scales,
+                             const int8_t *d_up_codes, const uint8_t *d_up_scales, int64_t rows, int64_t cols,
+                             int dtype, int act, void *d_dx, int64_t ld_dx, void *d_dup, int64_t ld_dup,
+                             ogq_stream_t stream);
+
+/*
+ * Weight and bias gradient of a linear layer (or 1x1 convolution, channels last) whose input is kept in 8 bits:
+ *   dW[o][i] = sum_t dy[t][o] x^[t][i],   db[o] = sum_t dy[t][o],   t < rows, i < cols, o < out_cols.
+ * d_dy [rows, out_cols] of type dtype with row stride ld_dy; d_dw fp32 [out_cols, cols], contiguous; d_db fp32 [out_cols] or NULL.
+ * accumulate = 0: the outputs are overwritten; 1: the sums are added to what they hold.  rows = 0 gives sums of 0.
+ * Products are exact and sums are fp32; the order of the additions depends on the sizes and the number of SMs only, so the same call
+ * gives the same bits again.  d_ws: scratch of ogq_act8_wgrad_workspace_bytes (a size for the current device), 256-byte aligned.
+ */
+size_t ogq_act8_wgrad_workspace_bytes(int64_t rows, int64_t cols, int64_t out_cols, int dtype);
+ogq_status ogq_act8_wgrad(const void *d_dy, int64_t ld_dy, const int8_t *d_codes, const uint8_t *d_scales,
+                          int64_t rows, int64_t cols, int64_t out_cols, int dtype, int accumulate, float *d_dw,
+                          float *d_db, void *d_ws, size_t ws_bytes, ogq_stream_t stream);
+
+/*
+ * Group norm with an activation, channels last.  x is [N, P, C] (samples, pixels or positions, channels), contiguous; the
+ * C channels form G groups of C / G neighbours (G = 1: one group per sample).  With mean and variance over the P * C/G values of a
+ * group of a sample, rstd = 1 / sqrt(variance + eps), xh = (x - mean) rstd:
+ *   forward   y = f(gamma_c xh + beta_c);  d_mean, d_rstd [N, G] fp32 are written for the backward pass.  d_gamma and d_beta fp32 [C],
+ *             each may be NULL (1 and 0).  d_codes and d_scales, both or neither: x kept in 8 bits, as the matrix [N P, C].
+ *   backward  from dy and either x itself (d_x, the code pointers NULL) or the kept x^ (d_x NULL), with mean and rstd of the forward pass:
+ *             dz = dy f'(gamma_c xh + beta_c),  dgamma_c = sum_{n,p} dz xh,  dbeta_c = sum_{n,p} dz,
+ *             dx = rstd (gamma_c dz - m1 - xh m2),  m1, m2 = the means of gamma dz and gamma dz xh over the group.
+ *             d_dgamma and d_dbeta fp32 [C], overwritten; each may be NULL.
+ * The variance is taken about the mean (no difference of large sums).  N, P or C may be 0 (sums over nothing are 0, so is the mean).
+ * G divides C, eps > 0.  P C/G is below 2^31 and N * ceil(C/32) * P below 2^31 (OGQ_ERR_UNSUPPORTED).  The order of the additions
+ * depends on the sizes and the number of SMs only.  d_ws: scratch of ogq_group_norm_workspace_bytes, 256-byte aligned.
+ * d_y may be d_x and d_dx may be d_dy; outputs overlap nothing else.
+ */
+size_t ogq_group_norm_workspace_bytes(int64_t N, int64_t P, int64_t C, int64_t G);
+ogq_status ogq_group_norm_forward(const void *d_x, int64_t N, int64_t P, int64_t C, int64_t G, int dtype,
+                                  const float *d_gamma, const float *d_beta, float eps, int act, int rounding,
+                                  uint64_t seed, uint32_t stream_id, void *d_y, float *d_mean, float *d_rstd,
+                                  int8_t *d_codes, uint8_t *d_scales, void *d_ws, size_t ws_bytes,
+                                  ogq_stream_t stream);
+ogq_status ogq_group_norm_backward(const void *d_dy, const void *d_x, const int8_t *d_codes,
+                                   const uint8_t *d_scales, int64_t N, int64_t P, int64_t C, int64_t G, int dtype,
+                                   const float *d_gamma, const float *d_beta, int act, const float *d_mean,
+                                   const float *d_rstd, void *d_dx, float *d_dgamma, float *d_dbeta, void *d_ws,
+                                   size_t ws_bytes, ogq_stream_t stream);
+
+/*
  * Measurement helpers (no counterpart in the paper; they do not touch the data path).
  * ogq_launch_count: number of kernels this library has launched in this process so far.
  * ogq_profile_enable(1): from now on every kernel launch of the library is bracketed by two CUDA

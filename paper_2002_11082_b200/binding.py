@@ -15,6 +15,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libogq.so")
 
 OGQ_BINGRAD_PB, OGQ_BINGRAD_B, OGQ_ORQ = 0, 1, 2
+OGQ_F32, OGQ_F16, OGQ_BF16 = 0, 1, 2
+OGQ_ACT_NONE, OGQ_ACT_RELU, OGQ_ACT_SILU, OGQ_ACT_GELU = 0, 1, 2, 3
+OGQ_ROUND_NEAREST, OGQ_ROUND_RANDOM = 0, 1
 OGQ_ST_EMPTY, OGQ_ST_NONFINITE, OGQ_ST_CONSTANT, OGQ_ST_ITER_CAP, OGQ_ST_INTERNAL = 1, 2, 4, 8, 16
 
 _STATUS_NAMES = {1: "OGQ_ERR_INVALID_ARG", 2: "OGQ_ERR_UNSUPPORTED", 3: "OGQ_ERR_WORKSPACE", 4: "OGQ_ERR_CUDA",
@@ -55,6 +58,12 @@ def lib() -> ctypes.CDLL:
         L.ogq_workspace_bytes.argtypes = [i32, i64, i32]
         L.ogq_bucket_packed_words.restype = i64
         L.ogq_bucket_packed_words.argtypes = [i64, i32, i32]
+        L.ogq_act8_groups.restype = i64
+        L.ogq_act8_groups.argtypes = [i64]
+        L.ogq_act8_wgrad_workspace_bytes.restype = sz
+        L.ogq_act8_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.ogq_group_norm_workspace_bytes.restype = sz
+        L.ogq_group_norm_workspace_bytes.argtypes = [i64, i64, i64, i64]
         L.ogq_dense_digits.restype = i32
         L.ogq_dense_digits.argtypes = [i32]
         L.ogq_dense_layout.restype = i32
@@ -79,6 +88,8 @@ _DATA_PATH = (
     "ogq_clip_threshold", "ogq_levels_orq_clipped", "ogq_levels_bingrad_clipped", "ogq_quant_error",
     "ogq_expected_error", "ogq_quantize_pack_dense", "ogq_unpack_sum_dense", "ogq_quantize_pack_clipped",
     "ogq_bucket_encode", "ogq_bucket_decode_sum",
+    "ogq_act8_encode", "ogq_act8_decode", "ogq_act8_forward", "ogq_act8_backward", "ogq_act8_wgrad",
+    "ogq_group_norm_forward", "ogq_group_norm_backward",
 )
 
 
@@ -163,6 +174,18 @@ def ogq_workspace_bytes(num_tensors: int, total_elems: int, max_levels: int) -> 
 
 def ogq_bucket_packed_words(total_elems: int, d: int, bits: int) -> int:
     return int(lib().ogq_bucket_packed_words(int(total_elems), int(d), int(bits)))
+
+
+def ogq_act8_groups(cols: int) -> int:
+    return int(lib().ogq_act8_groups(int(cols)))
+
+
+def ogq_act8_wgrad_workspace_bytes(rows: int, cols: int, out_cols: int, dtype: int) -> int:
+    return int(lib().ogq_act8_wgrad_workspace_bytes(int(rows), int(cols), int(out_cols), int(dtype)))
+
+
+def ogq_group_norm_workspace_bytes(N: int, P: int, C: int, G: int) -> int:
+    return int(lib().ogq_group_norm_workspace_bytes(int(N), int(P), int(C), int(G)))
 
 
 def ogq_dense_digits(s: int) -> int:

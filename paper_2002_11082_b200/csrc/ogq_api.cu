@@ -458,4 +458,207 @@ ogq_status ogq_bucket_decode_sum(const uint32_t* const* d_packed_k, const float*
     return e == cudaSuccess ? OGQ_OK : OGQ_ERR_CUDA;
 }
 
+namespace {
+
+bool valid_dtype(int d) { return d == OGQ_F32 || d == OGQ_F16 || d == OGQ_BF16; }
+bool valid_act(int a) { return a >= OGQ_ACT_NONE && a <= OGQ_ACT_GELU; }
+bool valid_rounding(int r) { return r == OGQ_ROUND_NEAREST || r == OGQ_ROUND_RANDOM; }
+bool aligned_to_type(const void* p, int dtype) { return ((uintptr_t)p & (dtype == OGQ_F32 ? 3u : 1u)) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+constexpr int64_t kMaxStride = (int64_t)1 << 40;  // rows * stride stays far inside 64 bits
+constexpr int64_t kMaxGroups = (int64_t)1 << 31;
+
+// OK, or why a matrix in 8 bits of this size is refused.
+ogq_status act8_sizes(int64_t rows, int64_t cols)
+{
+    if (rows < 0 || cols < 0) return OGQ_ERR_INVALID_ARG;
+    if (rows >= kMaxGroups || cols >= kMaxGroups) return OGQ_ERR_UNSUPPORTED;
+    return rows * ((cols + 31) / 32) < kMaxGroups ? OGQ_OK : OGQ_ERR_UNSUPPORTED;
+}
+
+bool valid_stride(int64_t ld, int64_t cols) { return ld >= cols && ld < kMaxStride; }
+
+}  // namespace
+
+int64_t ogq_act8_groups(int64_t cols) { return cols < 0 ? -1 : cols / 32 + (cols % 32 != 0); }
+
+ogq_status ogq_act8_encode(const void* d_x, int64_t ld_x, int64_t rows, int64_t cols, int dtype, int rounding,
+                           uint64_t seed, uint32_t stream_id, int8_t* d_codes, uint8_t* d_scales, ogq_stream_t stream)
+{
+    StageRange nvtx_range("ogq_act8_encode");
+    if (!valid_dtype(dtype) || !valid_rounding(rounding)) return OGQ_ERR_INVALID_ARG;
+    const ogq_status st = act8_sizes(rows, cols);
+    if (st != OGQ_OK) return st;
+    if (rows == 0 || cols == 0) return OGQ_OK;
+    if (!d_x || !d_codes || !d_scales || !aligned_to_type(d_x, dtype) || !valid_stride(ld_x, cols)) return OGQ_ERR_INVALID_ARG;
+    const int sms = sm_count_of_current_device();
+    if (sms <= 0) return OGQ_ERR_CUDA;
+    const ogq::Act8Forward a = {d_x, ld_x, nullptr, 0, rows, cols, dtype, OGQ_ACT_NONE, rounding, seed, stream_id, nullptr, 0,
+                                d_codes, d_scales, nullptr, nullptr};
+    return ogq::launch_act8_forward(a, sms, (cudaStream_t)stream) == cudaSuccess ? OGQ_OK : OGQ_ERR_CUDA;
+}
+
+ogq_status ogq_act8_decode(const int8_t* d_codes, const uint8_t* d_scales, int64_t rows, int64_t cols, int dtype,
+                           void* d_x, int64_t ld_x, ogq_stream_t stream)
+{
+    StageRange nvtx_range("ogq_act8_decode");
+    if (!valid_dtype(dtype)) return OGQ_ERR_INVALID_ARG;
+    const ogq_status st = act8_sizes(rows, cols);
+    if (st != OGQ_OK) return st;
+    if (rows == 0 || cols == 0) return OGQ_OK;
+    if (!d_x || !d_codes || !d_scales || !aligned_to_type(d_x, dtype) || !valid_stride(ld_x, cols)) return OGQ_ERR_INVALID_ARG;
+    const int sms = sm_count_of_current_device();
+    if (sms <= 0) return OGQ_ERR_CUDA;
+    const ogq::Act8Backward a = {nullptr, 0, d_codes, d_scales, nullptr, nullptr, rows, cols, dtype, OGQ_ACT_NONE, d_x, ld_x, nullptr, 0};
+    return ogq::launch_act8_backward(a, sms, (cudaStream_t)stream) == cudaSuccess ? OGQ_OK : OGQ_ERR_CUDA;
+}
+
+ogq_status ogq_act8_forward(const void* d_x, int64_t ld_x, const void* d_up, int64_t ld_up, int64_t rows, int64_t cols,
+                            int dtype, int act, int rounding, uint64_t seed, uint32_t stream_id, void* d_y, int64_t ld_y,
+                            int8_t* d_codes, uint8_t* d_scales, int8_t* d_up_codes, uint8_t* d_up_scales,
+                            ogq_stream_t stream)
+{
+    StageRange nvtx_range("ogq_act8_forward");
+    if (!valid_dtype(dtype) || !valid_act(act) || !valid_rounding(rounding)) return OGQ_ERR_INVALID_ARG;
+    const ogq_status st = act8_sizes(rows, cols);
+    if (st != OGQ_OK) return st;
+    if (rows == 0 || cols == 0) return OGQ_OK;
+    if (!d_x || !d_y || !d_codes || !d_scales || !aligned_to_type(d_x, dtype) || !aligned_to_type(d_y, dtype)) return OGQ_ERR_INVALID_ARG;
+    if (!valid_stride(ld_x, cols) || !valid_stride(ld_y, cols)) return OGQ_ERR_INVALID_ARG;
+    if (d_up) {
+        if (!d_up_codes || !d_up_scales || !aligned_to_type(d_up, dtype) || !valid_stride(ld_up, cols)) return OGQ_ERR_INVALID_ARG;
+    } else if (d_up_codes || d_up_scales) {
+        return OGQ_ERR_INVALID_ARG;
+    }
+    const int sms = sm_count_of_current_device();
+    if (sms <= 0) return OGQ_ERR_CUDA;
+    const ogq::Act8Forward a = {d_x, ld_x, d_up, ld_up, rows, cols, dtype, act, rounding, seed, stream_id, d_y, ld_y,
+                                d_codes, d_scales, d_up_codes, d_up_scales};
+    return ogq::launch_act8_forward(a, sms, (cudaStream_t)stream) == cudaSuccess ? OGQ_OK : OGQ_ERR_CUDA;
+}
+
+ogq_status ogq_act8_backward(const void* d_dy, int64_t ld_dy, const int8_t* d_codes, const uint8_t* d_scales,
+                             const int8_t* d_up_codes, const uint8_t* d_up_scales, int64_t rows, int64_t cols, int dtype,
+                             int act, void* d_dx, int64_t ld_dx, void* d_dup, int64_t ld_dup, ogq_stream_t stream)
+{
+    StageRange nvtx_range("ogq_act8_backward");
+    if (!valid_dtype(dtype) || !valid_act(act)) return OGQ_ERR_INVALID_ARG;
+    const ogq_status st = act8_sizes(rows, cols);
+    if (st != OGQ_OK) return st;
+    if (rows == 0 || cols == 0) return OGQ_OK;
+    if (!d_dy || !d_dx || !d_codes || !d_scales || !aligned_to_type(d_dy, dtype) || !aligned_to_type(d_dx, dtype)) return OGQ_ERR_INVALID_ARG;
+    if (!valid_stride(ld_dy, cols) || !valid_stride(ld_dx, cols)) return OGQ_ERR_INVALID_ARG;
+    if (d_dup) {
+        if (!d_up_codes || !d_up_scales || !aligned_to_type(d_dup, dtype) || !valid_stride(ld_dup, cols)) return OGQ_ERR_INVALID_ARG;
+    } else if (d_up_codes || d_up_scales) {
+        return OGQ_ERR_INVALID_ARG;
+    }
+    const int sms = sm_count_of_current_device();
+    if (sms <= 0) return OGQ_ERR_CUDA;
+    const ogq::Act8Backward a = {d_dy, ld_dy, d_codes, d_scales, d_up_codes, d_up_scales, rows, cols, dtype, act, d_dx, ld_dx, d_dup, ld_dup};
+    return ogq::launch_act8_backward(a, sms, (cudaStream_t)stream) == cudaSuccess ? OGQ_OK : OGQ_ERR_CUDA;
+}
+
+size_t ogq_act8_wgrad_workspace_bytes(int64_t rows, int64_t cols, int64_t out_cols, int dtype)
+{
+    if (!valid_dtype(dtype) || act8_sizes(rows, cols) != OGQ_OK || out_cols < 0 || out_cols >= kMaxGroups) return 0;
+    return ogq::ws_bytes_act8_wgrad(rows, cols, out_cols, dtype, sm_count_of_current_device()) + 256;
+}
+
+ogq_status ogq_act8_wgrad(const void* d_dy, int64_t ld_dy, const int8_t* d_codes, const uint8_t* d_scales, int64_t rows,
+                          int64_t cols, int64_t out_cols, int dtype, int accumulate, float* d_dw, float* d_db, void* d_ws,
+                          size_t ws_bytes, ogq_stream_t stream)
+{
+    StageRange nvtx_range("ogq_act8_wgrad");
+    if (!valid_dtype(dtype) || out_cols < 0 || (accumulate != 0 && accumulate != 1)) return OGQ_ERR_INVALID_ARG;
+    const ogq_status st = act8_sizes(rows, cols);
+    if (st != OGQ_OK) return st;
+    if (out_cols >= kMaxGroups) return OGQ_ERR_UNSUPPORTED;
+    if (out_cols == 0 || (cols == 0 && !d_db)) return OGQ_OK;
+    if (cols > 0 && (!d_dw || !aligned4(d_dw))) return OGQ_ERR_INVALID_ARG;
+    if (d_db && !aligned4(d_db)) return OGQ_ERR_INVALID_ARG;
+    if (rows > 0 && (!d_dy || !aligned_to_type(d_dy, dtype) || !valid_stride(ld_dy, out_cols))) return OGQ_ERR_INVALID_ARG;
+    if (rows > 0 && cols > 0 && (!d_codes || !d_scales)) return OGQ_ERR_INVALID_ARG;
+    const int sms = sm_count_of_current_device();
+    if (sms <= 0) return OGQ_ERR_CUDA;
+    if (!d_ws || ((uintptr_t)d_ws & 255u) || ws_bytes < ogq::ws_bytes_act8_wgrad(rows, cols, out_cols, dtype, sms)) return OGQ_ERR_WORKSPACE;
+    const ogq::Wgrad8 a = {d_dy, ld_dy, d_codes, d_scales, rows, cols, out_cols, dtype, accumulate, d_dw, d_db, d_ws};
+    return ogq::launch_act8_wgrad(a, sms, (cudaStream_t)stream) == cudaSuccess ? OGQ_OK : OGQ_ERR_CUDA;
+}
+
+static ogq_status group_norm_sizes(int64_t N, int64_t P, int64_t C, int64_t G)
+{
+    if (N < 0 || P < 0 || C < 0 || G < 1 || C % G != 0) return OGQ_ERR_INVALID_ARG;
+    if (N >= kMaxGroups || P >= kMaxGroups || C >= kMaxGroups) return OGQ_ERR_UNSUPPORTED;
+    if (P * (C / G) >= kMaxGroups) return OGQ_ERR_UNSUPPORTED;
+    const int64_t per_pixel = (C + 31) / 32;
+    if (P > 0 && N > 0 && per_pixel > 0 && (P >= kMaxGroups / N + 1 || N * P >= kMaxGroups || per_pixel >= kMaxGroups / (N * P) + 1 ||
+                                            N * P * per_pixel >= kMaxGroups))
+        return OGQ_ERR_UNSUPPORTED;
+    return OGQ_OK;
+}
+
+size_t ogq_group_norm_workspace_bytes(int64_t N, int64_t P, int64_t C, int64_t G)
+{
+    if (group_norm_sizes(N, P, C, G) != OGQ_OK) return 0;
+    return ogq::ws_bytes_group_norm(N, P, C, G) + 256;
+}
+
+ogq_status ogq_group_norm_forward(const void* d_x, int64_t N, int64_t P, int64_t C, int64_t G, int dtype,
+                                  const float* d_gamma, const float* d_beta, float eps, int act, int rounding, uint64_t seed,
+                                  uint32_t stream_id, void* d_y, float* d_mean, float* d_rstd, int8_t* d_codes,
+                                  uint8_t* d_scales, void* d_ws, size_t ws_bytes, ogq_stream_t stream)
+{
+    StageRange nvtx_range("ogq_group_norm_forward");
+    if (!valid_dtype(dtype) || !valid_act(act) || !valid_rounding(rounding) || !(eps > 0.f) || !(eps < 1e30f)) return OGQ_ERR_INVALID_ARG;
+    const ogq_status st = group_norm_sizes(N, P, C, G);
+    if (st != OGQ_OK) return st;
+    if ((d_codes != nullptr) != (d_scales != nullptr)) return OGQ_ERR_INVALID_ARG;
+    if (N == 0 || C == 0) return OGQ_OK;
+    if (!d_mean || !d_rstd || !aligned4(d_mean) || !aligned4(d_rstd) || !aligned4(d_gamma) || !aligned4(d_beta)) return OGQ_ERR_INVALID_ARG;
+    if (P > 0 && (!d_x || !d_y || !aligned_to_type(d_x, dtype) || !aligned_to_type(d_y, dtype))) return OGQ_ERR_INVALID_ARG;
+    if (!d_ws || ((uintptr_t)d_ws & 255u) || ws_bytes < ogq::ws_bytes_group_norm(N, P, C, G)) return OGQ_ERR_WORKSPACE;
+    const int sms = sm_count_of_current_device();
+    if (sms <= 0) return OGQ_ERR_CUDA;
+    ogq::GroupNorm a = {};
+    a.x = d_x; a.codes = d_codes; a.scales = d_scales;
+    a.N = N; a.P = P; a.C = C; a.G = G;
+    a.dtype = dtype; a.act = act; a.rounding = rounding;
+    a.gamma = d_gamma; a.beta = d_beta; a.eps = eps;
+    a.seed = seed; a.stream_id = stream_id;
+    a.out = d_y; a.mean = d_mean; a.rstd = d_rstd; a.ws = d_ws;
+    return ogq::launch_group_norm_forward(a, sms, (cudaStream_t)stream) == cudaSuccess ? OGQ_OK : OGQ_ERR_CUDA;
+}
+
+ogq_status ogq_group_norm_backward(const void* d_dy, const void* d_x, const int8_t* d_codes, const uint8_t* d_scales,
+                                   int64_t N, int64_t P, int64_t C, int64_t G, int dtype, const float* d_gamma,
+                                   const float* d_beta, int act, const float* d_mean, const float* d_rstd, void* d_dx,
+                                   float* d_dgamma, float* d_dbeta, void* d_ws, size_t ws_bytes, ogq_stream_t stream)
+{
+    StageRange nvtx_range("ogq_group_norm_backward");
+    if (!valid_dtype(dtype) || !valid_act(act)) return OGQ_ERR_INVALID_ARG;
+    const ogq_status st = group_norm_sizes(N, P, C, G);
+    if (st != OGQ_OK) return st;
+    if ((d_codes != nullptr) != (d_scales != nullptr) || (d_x && d_codes)) return OGQ_ERR_INVALID_ARG;
+    if (C == 0) return OGQ_OK;
+    if (!aligned4(d_gamma) || !aligned4(d_beta) || !aligned4(d_dgamma) || !aligned4(d_dbeta)) return OGQ_ERR_INVALID_ARG;
+    if (N > 0 && P > 0) {
+        if (!d_dy || !d_dx || !d_mean || !d_rstd || !aligned4(d_mean) || !aligned4(d_rstd)) return OGQ_ERR_INVALID_ARG;
+        if (!d_x && !d_codes) return OGQ_ERR_INVALID_ARG;
+        if (!aligned_to_type(d_dy, dtype) || !aligned_to_type(d_dx, dtype) || !aligned_to_type(d_x, dtype)) return OGQ_ERR_INVALID_ARG;
+    }
+    if (!d_ws || ((uintptr_t)d_ws & 255u) || ws_bytes < ogq::ws_bytes_group_norm(N, P, C, G)) return OGQ_ERR_WORKSPACE;
+    const int sms = sm_count_of_current_device();
+    if (sms <= 0) return OGQ_ERR_CUDA;
+    ogq::GroupNorm a = {};
+    a.x = d_x; a.dy = d_dy; a.codes = const_cast<int8_t*>(d_codes); a.scales = const_cast<uint8_t*>(d_scales);
+    a.N = N; a.P = P; a.C = C; a.G = G;
+    a.dtype = dtype; a.act = act;
+    a.gamma = d_gamma; a.beta = d_beta;
+    a.out = d_dx; a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
+    a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.ws = d_ws;
+    return ogq::launch_group_norm_backward(a, sms, (cudaStream_t)stream) == cudaSuccess ? OGQ_OK : OGQ_ERR_CUDA;
+}
+
 }  // extern "C"

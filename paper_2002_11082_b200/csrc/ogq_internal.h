@@ -62,4 +62,61 @@ cudaError_t launch_unpack_sum_dense(const uint32_t* const* d_packed_k, const flo
                                     const int64_t* d_off, const int64_t* d_packed_off, int T, int64_t total, int s,
                                     float scale, float* d_out, int sm_count, cudaStream_t stream);
 
+
+// activations in 8 bits (dtype, act and rounding as in ogq.h); d_y null: encode alone
+struct Act8Forward {
+    const void* x; int64_t ld_x;
+    const void* up; int64_t ld_up;
+    int64_t rows, cols;
+    int dtype, act, rounding;
+    uint64_t seed;
+    uint32_t stream_id;
+    void* y; int64_t ld_y;
+    int8_t* codes; uint8_t* scales;
+    int8_t* up_codes; uint8_t* up_scales;
+};
+cudaError_t launch_act8_forward(const Act8Forward& a, int sm_count, cudaStream_t stream);
+
+// dy null: decode x into dx (act is the identity)
+struct Act8Backward {
+    const void* dy; int64_t ld_dy;
+    const int8_t* codes; const uint8_t* scales;
+    const int8_t* up_codes; const uint8_t* up_scales;
+    int64_t rows, cols;
+    int dtype, act;
+    void* dx; int64_t ld_dx;
+    void* dup; int64_t ld_dup;
+};
+cudaError_t launch_act8_backward(const Act8Backward& a, int sm_count, cudaStream_t stream);
+
+struct Wgrad8 {
+    const void* dy; int64_t ld_dy;
+    const int8_t* codes; const uint8_t* scales;
+    int64_t rows, cols, out_cols;
+    int dtype, accumulate;
+    float* dw; float* db;
+    void* ws;
+};
+size_t ws_bytes_act8_wgrad(int64_t rows, int64_t cols, int64_t out_cols, int dtype, int sm_count);
+cudaError_t launch_act8_wgrad(const Wgrad8& a, int sm_count, cudaStream_t stream);
+
+struct GroupNorm {
+    const void* x;             // forward; backward from x itself
+    const void* dy;            // backward
+    int8_t* codes; uint8_t* scales;
+    int64_t N, P, C, G;
+    int dtype, act, rounding;
+    const float* gamma; const float* beta;
+    float eps;
+    uint64_t seed;
+    uint32_t stream_id;
+    void* out;                 // y or dx
+    float* mean; float* rstd;
+    float* dgamma; float* dbeta;
+    void* ws;
+};
+size_t ws_bytes_group_norm(int64_t N, int64_t P, int64_t C, int64_t G);
+cudaError_t launch_group_norm_forward(const GroupNorm& a, int sm_count, cudaStream_t stream);
+cudaError_t launch_group_norm_backward(const GroupNorm& a, int sm_count, cudaStream_t stream);
+
 }  // namespace ogq

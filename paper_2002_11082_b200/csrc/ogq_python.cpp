@@ -20,7 +20,7 @@ struct Arg {
     Kind kind;
 };
 
-constexpr int kMaxArgs = 17;
+constexpr int kMaxArgs = 24;
 
 struct Function {
     const char* name;
@@ -42,6 +42,12 @@ const Arg kGrad{"d_grad", kPtr}, kOff{"d_off", kPtr}, kT{"T", kInt}, kN{"total_e
     kStreamId{"stream_id", kU32}, kPackedOff{"d_packed_off", kPtr}, kPacked{"d_packed", kPtr}, kPackedK{"d_packed_k", kPtr},
     kLevelsK{"d_levels_k", kPtr}, kK{"K", kInt}, kScale{"scale", kFloat}, kOut{"d_out", kPtr}, kErr{"d_err", kPtr}, kD{"d", kInt},
     kStr{"stream", kStream};
+const Arg kX{"d_x", kPtr}, kLdX{"ld_x", kI64}, kUp{"d_up", kPtr}, kLdUp{"ld_up", kI64}, kRows{"rows", kI64}, kCols{"cols", kI64},
+    kDtype{"dtype", kInt}, kAct{"act", kInt}, kRounding{"rounding", kInt}, kY{"d_y", kPtr}, kLdY{"ld_y", kI64}, kCodes{"d_codes", kPtr},
+    kScales{"d_scales", kPtr}, kUpCodes{"d_up_codes", kPtr}, kUpScales{"d_up_scales", kPtr}, kDy{"d_dy", kPtr}, kLdDy{"ld_dy", kI64},
+    kDx{"d_dx", kPtr}, kLdDx{"ld_dx", kI64}, kDup{"d_dup", kPtr}, kLdDup{"ld_dup", kI64}, kSamples{"N", kI64}, kPixels{"P", kI64},
+    kChannels{"C", kI64}, kGroups{"G", kI64}, kGamma{"d_gamma", kPtr}, kBeta{"d_beta", kPtr}, kEps{"eps", kFloat}, kMean{"d_mean", kPtr},
+    kRstd{"d_rstd", kPtr}, kDgamma{"d_dgamma", kPtr}, kDbeta{"d_dbeta", kPtr};
 
 Function g_functions[] = {
     {"ogq_levels_bingrad", 12, {kGrad, kOff, kT, kN, kVariant, kLloyd, kLevels, kThresh, kStatus, kWs, kWsBytes, kStr}, nullptr},
@@ -59,6 +65,13 @@ Function g_functions[] = {
     {"ogq_quantize_pack_clipped", 14, {kGrad, kOff, kT, kN, kScheme, kS, kLevels, kThresh, kTau, kSeed, kStreamId, kPackedOff, kPacked, kStr}, nullptr},
     {"ogq_bucket_encode", 14, {kGrad, kN, kD, kScheme, kS, {"iters", kInt}, {"clip_c", kFloat}, kSeed, kStreamId, kLevels, kThresh, kStatus, kPacked, kStr}, nullptr},
     {"ogq_bucket_decode_sum", 9, {kPackedK, kLevelsK, kK, kN, kD, kS, kScale, kOut, kStr}, nullptr},
+    {"ogq_act8_encode", 11, {kX, kLdX, kRows, kCols, kDtype, kRounding, kSeed, kStreamId, kCodes, kScales, kStr}, nullptr},
+    {"ogq_act8_decode", 8, {kCodes, kScales, kRows, kCols, kDtype, kX, kLdX, kStr}, nullptr},
+    {"ogq_act8_forward", 18, {kX, kLdX, kUp, kLdUp, kRows, kCols, kDtype, kAct, kRounding, kSeed, kStreamId, kY, kLdY, kCodes, kScales, kUpCodes, kUpScales, kStr}, nullptr},
+    {"ogq_act8_backward", 15, {kDy, kLdDy, kCodes, kScales, kUpCodes, kUpScales, kRows, kCols, kDtype, kAct, kDx, kLdDx, kDup, kLdDup, kStr}, nullptr},
+    {"ogq_act8_wgrad", 14, {kDy, kLdDy, kCodes, kScales, kRows, kCols, {"out_cols", kI64}, kDtype, {"accumulate", kInt}, {"d_dw", kPtr}, {"d_db", kPtr}, kWs, kWsBytes, kStr}, nullptr},
+    {"ogq_group_norm_forward", 21, {kX, kSamples, kPixels, kChannels, kGroups, kDtype, kGamma, kBeta, kEps, kAct, kRounding, kSeed, kStreamId, kY, kMean, kRstd, kCodes, kScales, kWs, kWsBytes, kStr}, nullptr},
+    {"ogq_group_norm_backward", 20, {kDy, kX, kCodes, kScales, kSamples, kPixels, kChannels, kGroups, kDtype, kGamma, kBeta, kAct, kMean, kRstd, kDx, kDgamma, kDbeta, kWs, kWsBytes, kStr}, nullptr},
 };
 constexpr int kFunctions = sizeof(g_functions) / sizeof(g_functions[0]);
 
@@ -160,7 +173,14 @@ int call(int which, const Value* v)
         case 10: return invoke<P, P, I, L, I, P, U, W, P, P, P>(f, v);
         case 12: return invoke<P, P, I, L, I, I, P, P, P, U, W, P, P, P>(f, v);
         case 13: return invoke<P, L, I, I, I, I, F, U, W, P, P, P, P, P>(f, v);
-        default: return invoke<P, P, I, L, I, I, F, P, P>(f, v);
+        case 14: return invoke<P, P, I, L, I, I, F, P, P>(f, v);
+        case 15: return invoke<P, L, L, L, I, I, U, W, P, P, P>(f, v);
+        case 16: return invoke<P, P, L, L, I, P, L, P>(f, v);
+        case 17: return invoke<P, L, P, L, L, L, I, I, I, U, W, P, L, P, P, P, P, P>(f, v);
+        case 18: return invoke<P, L, P, P, P, P, L, L, I, I, P, L, P, L, P>(f, v);
+        case 19: return invoke<P, L, P, P, L, L, L, I, I, P, P, P, U, P>(f, v);
+        case 20: return invoke<P, L, L, L, L, I, P, P, F, I, I, U, W, P, P, P, P, P, P, U, P>(f, v);
+        default: return invoke<P, P, P, P, L, L, L, L, I, P, P, I, P, P, P, P, P, P, U, P>(f, v);
     }
 }
 
@@ -272,6 +292,13 @@ PyMethodDef g_methods[] = {
     ENTRY(12, "ogq_quantize_pack_clipped", "(d_grad, d_off, T, total_elems, scheme, s, d_levels, d_thresh, d_tau, seed, stream_id, d_packed_off, d_packed, stream=None)", "Quantize and pack the clipped gradient."),
     ENTRY(13, "ogq_bucket_encode", "(d_grad, total_elems, d, scheme, s, iters, clip_c, seed, stream_id, d_levels, d_thresh, d_status, d_packed, stream=None)", "Levels, quantize and pack of fixed-length buckets."),
     ENTRY(14, "ogq_bucket_decode_sum", "(d_packed_k, d_levels_k, K, total_elems, d, s, scale, d_out, stream=None)", "Unpack, dequantize and sum of fixed-length buckets."),
+    ENTRY(15, "ogq_act8_encode", "(d_x, ld_x, rows, cols, dtype, rounding, seed, stream_id, d_codes, d_scales, stream=None)", "Activations into 8 bits."),
+    ENTRY(16, "ogq_act8_decode", "(d_codes, d_scales, rows, cols, dtype, d_x, ld_x, stream=None)", "Activations back from 8 bits."),
+    ENTRY(17, "ogq_act8_forward", "(d_x, ld_x, d_up, ld_up, rows, cols, dtype, act, rounding, seed, stream_id, d_y, ld_y, d_codes, d_scales, d_up_codes, d_up_scales, stream=None)", "Activation function, with or without a gate, that keeps its inputs in 8 bits."),
+    ENTRY(18, "ogq_act8_backward", "(d_dy, ld_dy, d_codes, d_scales, d_up_codes, d_up_scales, rows, cols, dtype, act, d_dx, ld_dx, d_dup, ld_dup, stream=None)", "Backward pass of the activation function from its kept inputs."),
+    ENTRY(19, "ogq_act8_wgrad", "(d_dy, ld_dy, d_codes, d_scales, rows, cols, out_cols, dtype, accumulate, d_dw, d_db, d_ws, ws_bytes, stream=None)", "Weight and bias gradient of a linear layer from its kept input."),
+    ENTRY(20, "ogq_group_norm_forward", "(d_x, N, P, C, G, dtype, d_gamma, d_beta, eps, act, rounding, seed, stream_id, d_y, d_mean, d_rstd, d_codes, d_scales, d_ws, ws_bytes, stream=None)", "Group norm with an activation, channels last; may keep its input in 8 bits."),
+    ENTRY(21, "ogq_group_norm_backward", "(d_dy, d_x, d_codes, d_scales, N, P, C, G, dtype, d_gamma, d_beta, act, d_mean, d_rstd, d_dx, d_dgamma, d_dbeta, d_ws, ws_bytes, stream=None)", "Backward pass of the group norm, from its input or from what was kept of it."),
     {"setup", setup, METH_VARARGS, nullptr},
     {"set_addresses", set_addresses, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
