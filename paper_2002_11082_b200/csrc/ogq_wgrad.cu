@@ -1,70 +1,757 @@
 // Weight and bias gradient of a linear layer from its input kept in 8 bits: dW = dy^T x^, db = sum of dy's rows.
+//   dW[o][i] = sum_t dy[t][o] x^[t][i]:  a product whose summed index t is the row of both operands.  x^ = code * 2^e is a bf16
+// number, so nothing is lost by multiplying in bf16: dy in bf16 goes to the tensor cores as it is, dy in fp16 and fp32 as the sum
+// of two and three bf16 terms (8 + 3 and 8 + 8 + 8 bits), stacked along t.
+//   A pair of CTAs works on a tile of 256 x BN weights, 64 rows of t at a time: TMA brings dy's tile (swizzled, the operand as it lies
+// in memory) and the codes; four warps turn the codes into bf16 in shared memory (5 instructions for two values); one thread issues
+// the MMAs of both CTAs.  Pairs: each SM holds half of x^'s tile, so every code is converted once for 256 columns of dy, and both
+// operands cost half the shared memory traffic of single CTAs.
+//   The tensor cores cut, not round, what they add to a running sum, which drifts by 2^-24 a step: a sum over 16,384 rows came out
+// 9e-6 off, one over 1,024 rows 1e-6.  So a running sum is taken out of TMEM after kFlush * 64 rows and added in registers, rounded to
+// nearest, while the next one grows in the other half of TMEM.
+//   Work is split by tile as long as there are tiles for all pairs; what is left (all of it, when weights are few and rows many) by
+// steps of 64 rows, partial tiles joined by a second kernel in a fixed order.
+#include <cuda.h>
+
 #include "ogq_act8.cuh"
 #include "ogq_internal.h"
+#include "ogq_tcgen05.cuh"
 
 namespace ogq {
 
-struct WgArgs {
-    const void* dy; int64_t ld_dy;
-    const int8_t* codes; const uint8_t* scales;
-    int64_t rows, cols, out_cols;
-    float* dw; float* db;
-    bool accumulate;
+constexpr int kStepRows = 64;                  // rows of t per stage
+constexpr int kFlush = 8;                      // stages per running sum
+constexpr int kWgStages = 5;
+constexpr int kTileM = 256;                    // columns of dy per tile (both CTAs)
+constexpr int kABytes = 128 * kStepRows * 2;   // dy's tile of one CTA
+constexpr int kWgThreads = 512;                // a warpgroup for TMA, MMA and TMEM; one of converters; two that take sums out of TMEM
+// Registers a thread of the three kinds; the block starts with 512 * 128 = 65,536, which the split must not exceed.
+constexpr int kRegsControl = 40, kRegsConvert = 104, kRegsSums = 184;
+static_assert(128 * kRegsControl + 128 * kRegsConvert + 256 * kRegsSums <= kWgThreads * 128, "a warpgroup would wait for registers for ever");
+constexpr uint32_t kTmemColumns = 512;
+constexpr int kMinSteps = 8;                   // fewer steps than these are not split: a second launch costs more than they do
+
+template <int BN> struct WgShape {
+    static constexpr int kCols = BN / 2;                          // columns of x^ that one CTA converts
+    static constexpr int kOcts = kCols / 8;                       // a converter thread has eight of them, in
+    static constexpr int kRowsAtOnce = 128 / kOcts;               // rows row, row + kRowsAtOnce, ...
+    static constexpr int kRowsEach = kStepRows / kRowsAtOnce;
+    static constexpr int kBBytes = kCols * kStepRows * 2;
+    static constexpr int kRawBytes = kCols * kStepRows;
+    static constexpr int kStageBytes = kABytes + kBBytes + kRawBytes;
+    static constexpr int kSmem = kWgStages * kStageBytes + 1024;  // + alignment to the swizzle's 1024 bytes
+    static constexpr int kSlotFloats = 128 * BN;                  // a partial tile of one CTA
 };
 
-// A tile of 32 x 32 weights per CTA, 32 rows at a time.
-template <class E>
-__global__ void __launch_bounds__(kThreads) k_wgrad_any(const __grid_constant__ WgArgs a)
-{
-    pdl_wait();
-    pdl_launch_dependents();
-    __shared__ float dy[32][33], x[32][33];
-    const int64_t tiles = a.cols > 0 ? (a.cols + 31) / 32 : 1;  // no columns: the bias alone
-    const int64_t o0 = blockIdx.x / tiles * 32, i0 = (blockIdx.x - o0 / 32 * tiles) * 32;
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, bias[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t t0 = 0; t0 < a.rows; t0 += 32) {
-        for (int k = ty; k < 32; k += 8) {
-            const int64_t t = t0 + k;
-            dy[k][tx] = t < a.rows && o0 + tx < a.out_cols ? load1((const E*)a.dy + t * a.ld_dy + o0 + tx) : 0.f;
-            x[k][tx] = t < a.rows && i0 + tx < a.cols
-                           ? (float)a.codes[t * a.cols + i0 + tx] * act8_unit(a.scales[t * act8_groups(a.cols) + (i0 + tx) / kAct8Group]) : 0.f;
-        }
-        __syncthreads();
-        for (int k = 0; k < 32; ++k) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                acc[j] = __fmaf_rn(dy[k][ty * 4 + j], x[k][tx], acc[j]);
-                bias[j] += dy[k][ty * 4 + j];
-            }
-        }
-        __syncthreads();
+struct WgArgs {
+    const uint8_t* scales;
+    float* dw;
+    float* slots;
+    int64_t cols, out_cols;
+    int64_t rows;       // of this launch
+    int groups;         // of a row
+    int tiles_m, tiles_n;
+    int steps;          // of a tile: terms * steps_x
+    int steps_x;        // 64-row steps of x^
+    int pairs;
+    int whole;          // tiles per pair that are done alone
+    int64_t rest;       // steps of the tiles left
+    int64_t per;        // of them per pair
+    bool accumulate;
+    bool wide;          // 32-byte stores
+};
+
+// The pieces of work of one pair: (tile, steps [k0, k1)), the same sequence in every role.
+struct WgWork {
+    int i;
+    int64_t at, end;
+    int tile, k0, k1, slot;  // slot < 0: the whole sum
+    __device__ __forceinline__ WgWork(const WgArgs& a, int pair) : i(0), tile(0), k0(0), k1(0), slot(-1)
+    {
+        at = (int64_t)pair * a.per;
+        if (at > a.rest) at = a.rest;
+        end = at + a.per < a.rest ? at + a.per : a.rest;
+        first_ = true;
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t o = o0 + ty * 4 + j;
-        if (o >= a.out_cols) break;
-        if (i0 + tx < a.cols) {
-            float* w = a.dw + o * a.cols + i0 + tx;
-            *w = a.accumulate ? *w + acc[j] : acc[j];
+    __device__ __forceinline__ bool next(const WgArgs& a, int pair)
+    {
+        if (i < a.whole) {
+            tile = pair + i * a.pairs;
+            k0 = 0;
+            k1 = a.steps;
+            ++i;
+            return true;
         }
-        if (a.db && i0 == 0 && tx == 0) a.db[o] = a.accumulate ? a.db[o] + bias[j] : bias[j];
+        if (at >= end) return false;
+        const int j = (int)(at / a.steps);
+        tile = a.whole * a.pairs + j;
+        k0 = (int)(at - (int64_t)j * a.steps);
+        const int64_t left = end - at;
+        k1 = (int)(k0 + left < a.steps ? k0 + left : a.steps);
+        slot = k0 == 0 && k1 == a.steps ? -1 : first_ ? 0 : 1;
+        first_ = false;
+        at += k1 - k0;
+        return true;
+    }
+    bool first_;
+};
+
+// Tiles in columns of eight: those that run side by side read few different rows of both operands.
+__device__ __forceinline__ void wg_tile_place(int tile, int tiles_m, int tiles_n, int& m, int& n)
+{
+    const int band = tile / (8 * tiles_n), in = tile - band * 8 * tiles_n;
+    const int height = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+    n = in / height;
+    m = band * 8 + in - n * height;
+}
+
+// Two codes of a word, already spread to the low bytes of its halves, times the unit: 128 + (low seven bits) less 128, or 256
+// where the sign is set, both bf16 numbers whose bits are an OR away.
+__device__ __forceinline__ uint32_t wg_value2(uint32_t p, __nv_bfloat162 unit)
+{
+    const uint32_t a = (p & 0x007f007fu) | 0x43004300u, b = (p & 0x00800080u) | 0x43004300u;
+    const __nv_bfloat162 q = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    const __nv_bfloat162 v = __hmul2(q, unit);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// The scale bytes of this thread's rows of a step.
+template <int BN>
+__device__ __forceinline__ void wg_scales(const WgArgs& a, int step_x, int row, int group, uint32_t (&s)[WgShape<BN>::kRowsEach])
+{
+#pragma unroll
+    for (int j = 0; j < WgShape<BN>::kRowsEach; ++j) {
+        const int64_t t = (int64_t)step_x * kStepRows + row + WgShape<BN>::kRowsAtOnce * j;
+        s[j] = t < a.rows && group < a.groups ? (uint32_t)a.scales[t * a.groups + group] : 0u;
     }
 }
 
-size_t ws_bytes_act8_wgrad(int64_t, int64_t, int64_t, int, int) { return 0; }
-
-cudaError_t launch_act8_wgrad(const Wgrad8& p, int, cudaStream_t stream)
+// This thread's rows, eight codes each: `raw` and `b` are this stage's, oct the thread's eight columns.  Eight lanes write the 128
+// bytes of a row of a swizzled block: no bank conflicts.
+template <int BN>
+__device__ __forceinline__ void wg_convert(uint32_t raw, uint32_t b, int row, int oct, const uint32_t (&s)[WgShape<BN>::kRowsEach])
 {
-    WgArgs a = {p.dy, p.ld_dy, p.codes, p.scales, p.rows, p.cols, p.out_cols, p.dw, p.db, p.accumulate != 0};
-    const int64_t tiles = p.cols > 0 ? (p.cols + 31) / 32 : 1;
-    const int64_t ctas = tiles * ((p.out_cols + 31) / 32);
-    if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
+    constexpr int kCols = WgShape<BN>::kCols;
+#pragma unroll
+    for (int j = 0; j < WgShape<BN>::kRowsEach; ++j) {
+        const int t = row + WgShape<BN>::kRowsAtOnce * j;
+        uint32_t x, y;
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(raw + t * kCols + oct * 8));
+        const uint32_t u = s[j] << 7 | s[j] << 23;
+        const __nv_bfloat162 unit = *reinterpret_cast<const __nv_bfloat162*>(&u);
+        const uint32_t v0 = wg_value2(__byte_perm(x, 0, 0x4140), unit), v1 = wg_value2(__byte_perm(x, 0, 0x4342), unit);
+        const uint32_t v2 = wg_value2(__byte_perm(y, 0, 0x4140), unit), v3 = wg_value2(__byte_perm(y, 0, 0x4342), unit);
+        const uint32_t at = b + (oct >> 3) * (kStepRows * 128) + t * 128 + (((oct ^ t) & 7) << 4);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(at), "r"(v0), "r"(v1), "r"(v2), "r"(v3) : "memory");
+    }
+}
+
+__device__ __forceinline__ void store8_wide(float* p, const float* v)
+{
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 :: "l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}
+
+// Eight neighbouring weights of row o from column i on.
+__device__ __forceinline__ void wg_store8(const WgArgs& a, int64_t o, int64_t i, float (&v)[8])
+{
+    if (o >= a.out_cols || i >= a.cols) return;
+    float* w = a.dw + o * a.cols + i;
+    if (a.wide) {  // cols is a multiple of 8
+        if (a.accumulate) {
+            const float4 p = *reinterpret_cast<const float4*>(w), q = *reinterpret_cast<const float4*>(w + 4);
+            v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
+            v[4] += q.x; v[5] += q.y; v[6] += q.z; v[7] += q.w;
+        }
+        store8_wide(w, v);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i + j < a.cols) w[j] = a.accumulate ? w[j] + v[j] : v[j];
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kWgThreads, 1) __cluster_dims__(2, 1, 1)
+k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ WgArgs a)
+{
+    using S = WgShape<BN>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[4 * kWgStages + 4];
+    __shared__ uint32_t tmem_base;
+    __shared__ volatile int failed;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int pair = (int)(blockIdx.x >> 1);
+    const uint32_t bar0 = smem_u32(bars);
+    // empty: the stage's MMAs are done (both CTAs).  raw: the codes are here.  dy (leader's): both CTAs' tiles of dy are here.
+    // ready (leader's): both CTAs' codes are converted.  sum: a running sum is complete (both).  taken (leader's): it has been read.
+    const auto empty = [&](int s) { return bar0 + 8u * s; };
+    const auto raw = [&](int s) { return bar0 + 8u * (kWgStages + s); };
+    const auto dyb = [&](int s) { return bar0 + 8u * (2 * kWgStages + s); };
+    const auto ready = [&](int s) { return bar0 + 8u * (3 * kWgStages + s); };
+    const auto sum = [&](int d) { return bar0 + 8u * (4 * kWgStages + d); };
+    const auto taken = [&](int d) { return bar0 + 8u * (4 * kWgStages + 2 + d); };
+    const auto stage_a = [&](int s) { return base + s * S::kStageBytes; };
+    const auto stage_b = [&](int s) { return base + s * S::kStageBytes + kABytes; };
+    const auto stage_raw = [&](int s) { return base + s * S::kStageBytes + kABytes + S::kBBytes; };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kWgStages; ++s) {
+            mbar_init(empty(s), 1);
+            mbar_init(raw(s), 1);
+            mbar_init(dyb(s), 1);
+            mbar_init(ready(s), 8);
+        }
+        for (int d = 0; d < 2; ++d) {
+            mbar_init(sum(d), 1);
+            mbar_init(taken(d), 16);
+        }
+        failed = 0;
+        mbar_init_fence();
+        tma_prefetch_map(&map_dy);
+        tma_prefetch_map(&map_x);
+    }
+    if (warp == 2) tmem_alloc_pair(smem_u32(&tmem_base), kTmemColumns);
+    tcgen05_fence_before();
+    cluster_sync();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_base;
+    pdl_wait();
+    pdl_launch_dependents();
+
+    if (warp < 4) {
+        fewer_registers<kRegsControl>();
+        if (warp == 0 && lane == 0) {  // TMA
+            WgWork w(a, pair);
+            int s = 0;
+            uint32_t phase = 1;  // the first pass over the stages finds them empty
+            bool ok = true;
+            while (ok && w.next(a, pair)) {
+                int m, n;
+                wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
+                const int o = m * kTileM + (int)rank * 128, i = n * BN + (int)rank * S::kCols;
+                for (int k = w.k0; k < w.k1; ++k) {
+                    if (!(ok = mbar_wait(empty(s), phase, &failed))) break;
+                    const uint32_t dy_bar = map_to(dyb(s), 0);
+                    if (rank == 0) mbar_expect(dyb(s), 2 * kABytes);
+                    mbar_expect(raw(s), S::kRawBytes);
+                    tma_load_pair(stage_raw(s), &map_x, i, k % a.steps_x * kStepRows, raw(s));
+                    tma_load_pair(stage_a(s), &map_dy, o, k * kStepRows, dy_bar);
+                    tma_load_pair(stage_a(s) + kABytes / 2, &map_dy, o + 64, k * kStepRows, dy_bar);
+                    if (++s == kWgStages) { s = 0; phase ^= 1; }
+                }
+            }
+            // Until the last copies have landed: a stage is free again when its MMAs, and so its copies, are done.
+            for (int k = 0; k < kWgStages; ++k) {
+                if (!mbar_wait(empty(s), phase, &failed)) break;
+                if (++s == kWgStages) { s = 0; phase ^= 1; }
+            }
+        } else if (warp == 1 && lane == 0 && rank == 0) {  // MMA of both CTAs
+            WgWork w(a, pair);
+            int s = 0, d = 0;
+            uint32_t phase = 0, dphase = 1;
+            bool ok = true;
+            constexpr uint32_t instruction = instruction_bf16(kTileM, BN);
+            while (ok && w.next(a, pair)) {
+                for (int k = w.k0; ok && k < w.k1; k += kFlush) {
+                    const int last = k + kFlush < w.k1 ? k + kFlush : w.k1;
+                    if (!(ok = mbar_wait(taken(d), dphase, &failed))) break;
+                    tcgen05_fence_after();
+                    for (int q = k; q < last; ++q) {
+                        if (!(ok = mbar_wait(dyb(s), phase, &failed) && mbar_wait(ready(s), phase, &failed))) break;
+                        tcgen05_fence_after();
+                        const uint64_t da = tile_descriptor(stage_a(s), kStepRows * 128), db = tile_descriptor(stage_b(s), kStepRows * 128);
+#pragma unroll
+                        for (int j = 0; j < kStepRows / 16; ++j)  // 16 rows are 2048 bytes on
+                            mma_bf16_pair(tmem + d * BN, da + j * (2048 >> 4), db + j * (2048 >> 4), instruction, q > k || j > 0);
+                        mma_commit_pair(empty(s));
+                        if (++s == kWgStages) { s = 0; phase ^= 1; }
+                    }
+                    if (!ok) break;
+                    mma_commit_pair(sum(d));
+                    if (++d == 2) { d = 0; dphase ^= 1; }
+                }
+            }
+        }
+    } else if (warp < 8) {  // converters
+        fewer_registers<kRegsConvert>();
+        const int id = threadIdx.x - 128;
+        const int oct = id % S::kOcts, row = id / S::kOcts;
+        WgWork w(a, pair);
+        int s = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        const auto step = [&](const uint32_t (&u)[S::kRowsEach]) {
+            if (!(ok = __all_sync(0xffffffffu, mbar_wait(raw(s), phase, &failed)))) return;
+            wg_convert<BN>(stage_raw(s), stage_b(s), row, oct, u);
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to(ready(s), 0));
+            if (++s == kWgStages) { s = 0; phase ^= 1; }
+        };
+        while (ok && w.next(a, pair)) {
+            int m, n;
+            wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
+            const int group = (n * BN + (int)rank * S::kCols) / kAct8Group + oct / 4;
+            uint32_t u[S::kRowsEach], v[S::kRowsEach];  // scales two steps ahead: they come from L2 or memory
+            wg_scales<BN>(a, w.k0 % a.steps_x, row, group, u);
+            if (w.k0 + 1 < w.k1) wg_scales<BN>(a, (w.k0 + 1) % a.steps_x, row, group, v);
+            for (int k = w.k0; ok && k < w.k1; k += 2) {
+                step(u);
+                if (k + 2 < w.k1) wg_scales<BN>(a, (k + 2) % a.steps_x, row, group, u);
+                if (!ok || k + 1 >= w.k1) break;
+                step(v);
+                if (k + 3 < w.k1) wg_scales<BN>(a, (k + 3) % a.steps_x, row, group, v);
+            }
+        }
+    } else {  // sums out of TMEM, and out
+        more_registers<kRegsSums>();
+        constexpr int kHalf = BN / 2;
+        const int quarter = warp & 3, half = (warp - 8) >> 2;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        WgWork w(a, pair);
+        int d = 0;
+        uint32_t dphase = 0;
+        bool ok = true;
+        while (ok && w.next(a, pair)) {
+            float acc[kHalf];
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j) acc[j] = 0.f;
+            for (int k = w.k0; k < w.k1; k += kFlush) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(sum(d), dphase, &failed)))) break;
+                tcgen05_fence_after();
+#pragma unroll
+                for (int c = 0; c < kHalf; c += 16) {
+                    float v[16];
+                    tmem_load16(tmem + lanes + d * BN + half * kHalf + c, v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[c + j] = __fadd_rn(acc[c + j], v[j]);
+                }
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to(taken(d), 0));
+                if (++d == 2) { d = 0; dphase ^= 1; }
+            }
+            if (!ok) {
+#pragma unroll
+                for (int j = 0; j < kHalf; ++j) acc[j] = __uint_as_float(0x7fc00000u);  // a wait that ran out is not to be missed
+            }
+            int m, n;
+            wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
+            const int row = quarter * 32 + lane;
+            if (w.slot < 0) {
+                const int64_t o = (int64_t)m * kTileM + rank * 128 + row, i = (int64_t)n * BN + half * kHalf;
+#pragma unroll
+                for (int c = 0; c < kHalf; c += 8) {
+                    float v[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = acc[c + j];
+                    wg_store8(a, o, i + c, v);
+                }
+            } else {
+                float* slot = a.slots + ((int64_t)(pair * 2 + w.slot) * 2 + rank) * S::kSlotFloats;
+#pragma unroll
+                for (int c = 0; c < kHalf; c += 8) store8_wide(slot + ((half * kHalf + c) / 8 * 128 + row) * 8, acc + c);
+            }
+        }
+    }
+    __syncwarp();
+    tcgen05_fence_before();
+    cluster_sync();
+    tcgen05_fence_after();
+    if (warp == 2) tmem_free_pair(tmem, kTmemColumns);
+}
+
+// Joins the partial tiles: eight weights a thread; PARTS > 1: many pairs' parts of few tiles, each PARTS-th summed by another
+// warp of the CTA, then in order.  A CTA takes 256 / PARTS rows of eight columns.
+template <int BN, int PARTS>
+__global__ void __launch_bounds__(kThreads) k_wgrad_join(const __grid_constant__ WgArgs a)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr int kRows = kThreads / PARTS;  // of the tile's 256 x BN/8 pieces (CTA-of-the-pair, octet, row)
+    __shared__ float4 sh[PARTS > 1 ? PARTS : 1][PARTS > 1 ? kRows : 1][2];
+    constexpr int kPerTile = 256 * (BN / 8) / kRows;
+    const int j = blockIdx.x / kPerTile;
+    const int part = threadIdx.x / kRows, r = threadIdx.x - part * kRows;
+    const int piece = (blockIdx.x - j * kPerTile) * kRows + r;
+    const int rank = piece / (128 * (BN / 8)), in = piece - rank * (128 * (BN / 8));
+    const int oct = in / 128, row = in - oct * 128;
+    const int64_t first = (int64_t)j * a.steps / a.per, last = ((int64_t)(j + 1) * a.steps - 1) / a.per;
+    if (first == last) return;  // done by one pair
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int64_t p = first + part; p <= last; p += PARTS) {
+        const int slot = p * a.per / a.steps == j ? 0 : 1;
+        const float4* s = reinterpret_cast<const float4*>(a.slots + ((p * 2 + slot) * 2 + rank) * WgShape<BN>::kSlotFloats + (int64_t)in * 8);
+        const float4 x = __ldcg(s), y = __ldcg(s + 1);
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+        v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+    }
+    if constexpr (PARTS > 1) {
+        sh[part][r][0] = make_float4(v[0], v[1], v[2], v[3]);
+        sh[part][r][1] = make_float4(v[4], v[5], v[6], v[7]);
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int q = 1; q < PARTS; ++q) {
+            const float4 x = sh[q][r][0], y = sh[q][r][1];
+            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+            v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+        }
+    }
+    int m, n;
+    wg_tile_place(a.whole * a.pairs + j, a.tiles_m, a.tiles_n, m, n);
+    wg_store8(a, (int64_t)m * kTileM + rank * 128 + row, (int64_t)n * BN + oct * 8, v);
+}
+
+// ---------------------------------------------------------------------------
+// Operands that TMA cannot read as they are (fp16, fp32, rows off 16-byte boundaries) are laid out in the scratch first:
+// dy as bf16 terms stacked along t, each of `padded` rows (a multiple of 64, zeros behind the last), and the codes with rows of
+// a multiple of 16 bytes.
+// ---------------------------------------------------------------------------
+struct WgLayout {
+    const void* dy; int64_t ld_dy;
+    const int8_t* codes;
+    uint16_t* terms; int64_t ld_terms;   // null: dy is read as it is
+    int8_t* kept; int64_t ld_kept;       // null: the codes are
+    int64_t rows, padded, cols, out_cols;
+};
+
+// Cut, not rounded, so that the largest fp32 numbers do not become infinite; what is left is exact.  Infinities and NaN have a
+// first term only.
+template <int TERMS>
+__device__ __forceinline__ void wg_split(float v, uint16_t (&t)[TERMS])
+{
+    const bool finite = (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) {
+        uint32_t b = __float_as_uint(v);
+        if (k == 0 && !finite && (b & 0x007fffffu)) b |= 0x00400000u;  // a NaN stays one when cut
+        t[k] = (uint16_t)(k > 0 && !finite ? 0u : b >> 16);
+        v = __fsub_rn(v, __uint_as_float(b & 0xffff0000u));
+    }
+}
+
+template <class E, int TERMS>
+__global__ void __launch_bounds__(kThreads) k_wgrad_layout(const __grid_constant__ WgLayout a)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t stride = (int64_t)gridDim.x * kThreads, id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (a.terms) {
+        const int64_t octs = a.ld_terms / 8, n = a.padded * octs;
+        for (int64_t i = id; i < n; i += stride) {
+            const int64_t t = i / octs, c = (i - t * octs) * 8;
+            uint16_t v[8][TERMS];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) wg_split<TERMS>(t < a.rows && c + j < a.out_cols ? load1((const E*)a.dy + t * a.ld_dy + c + j) : 0.f, v[j]);
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k)
+                *reinterpret_cast<uint4*>(a.terms + (k * a.padded + t) * a.ld_terms + c) =
+                    make_uint4(v[0][k] | (uint32_t)v[1][k] << 16, v[2][k] | (uint32_t)v[3][k] << 16, v[4][k] | (uint32_t)v[5][k] << 16,
+                               v[6][k] | (uint32_t)v[7][k] << 16);
+        }
+    }
+    if (a.kept) {
+        const int64_t pieces = a.ld_kept / 16, n = a.rows * pieces;
+        for (int64_t i = id; i < n; i += stride) {
+            const int64_t t = i / pieces, c = (i - t * pieces) * 16;
+            uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (c + j < a.cols) w[j / 4] |= (uint32_t)(uint8_t)a.codes[t * a.cols + c + j] << (j % 4 * 8);
+            *reinterpret_cast<uint4*>(a.kept + t * a.ld_kept + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Bias: a CTA sums V columns a lane over its rows; several chunks of rows leave partial sums for the second kernel.
+// ---------------------------------------------------------------------------
+struct WgBias {
+    const void* dy; int64_t ld_dy;
+    int64_t rows, out_cols, chunk;
+    float* part; float* db;
+    int chunks, ctiles;
+    bool accumulate;
+};
+
+template <class E, int V>
+__global__ void __launch_bounds__(kThreads) k_wgrad_bias(const __grid_constant__ WgBias a)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    __shared__ float sh[kWarps][32 * V];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t k = blockIdx.x / a.ctiles, c = ((blockIdx.x - k * a.ctiles) * 32 + lane) * V;
+    const int64_t end = (k + 1) * a.chunk < a.rows ? (k + 1) * a.chunk : a.rows;
+    float s[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = 0.f;
+    if (c < a.out_cols) {
+        for (int64_t t = k * a.chunk + warp; t < end; t += kWarps) {
+            float v[V];
+            if constexpr (V == 8) unpack8(load_raw8((const E*)a.dy + t * a.ld_dy + c), v);
+            else v[0] = load1((const E*)a.dy + t * a.ld_dy + c);
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] = __fadd_rn(s[j], v[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) sh[warp][lane * V + j] = s[j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * V; i += kThreads) {
+        const int64_t o = (blockIdx.x - k * a.ctiles) * 32 * V + i;
+        if (o >= a.out_cols) break;
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) sum += sh[w][i];
+        if (a.chunks == 1) a.db[o] = a.accumulate ? a.db[o] + sum : sum;
+        else a.part[k * a.out_cols + o] = sum;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) k_wgrad_bias_join(const __grid_constant__ WgBias a)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t o = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (o >= a.out_cols) return;
+    double s = 0.0;
+    for (int k = 0; k < a.chunks; ++k) s += (double)__ldcg(a.part + (int64_t)k * a.out_cols + o);
+    a.db[o] = a.accumulate ? (float)((double)a.db[o] + s) : (float)s;
+}
+
+// All sums empty.
+__global__ void __launch_bounds__(kThreads) k_wgrad_zero(float* p, int64_t n, float* q, int64_t m)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t stride = (int64_t)gridDim.x * kThreads;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n + m; i += stride) {
+        if (i < n) p[i] = 0.f;
+        else q[i - n] = 0.f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int64_t kLayoutBytes = (int64_t)40 << 20;  // of operands laid out at a time: they stay in L2 until they are read
+constexpr int kBiasCtas = 4;                         // per SM
+
+int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+int terms_of(int dtype) { return dtype == OGQ_F32 ? 3 : dtype == OGQ_F16 ? 2 : 1; }
+
+struct Plan {
+    bool lay_dy, lay_x;
+    int terms, pairs;
+    int64_t ld_terms, ld_kept, rows;  // rows per launch
+    int64_t slots_bytes, bias_bytes, terms_bytes, kept_bytes;
+    int64_t bias_chunk;
+    int bias_chunks;
+};
+
+// Laid out or not is decided by the call's addresses; the scratch is sized for the worse.
+Plan make_plan(int64_t rows, int64_t cols, int64_t out_cols, int dtype, bool lay_dy, bool lay_x, int sm_count)
+{
+    Plan p = {};
+    p.lay_dy = lay_dy;
+    p.lay_x = lay_x;
+    p.terms = terms_of(dtype);
+    p.pairs = sm_count / 2;
+    p.ld_terms = up_to(out_cols, 8);
+    p.ld_kept = up_to(cols, 16);
+    p.rows = rows;
+    if (lay_dy || lay_x) {
+        const int64_t per_row = (lay_dy ? p.terms * p.ld_terms * 2 : 0) + (lay_x ? p.ld_kept : 0);
+        int64_t most = kLayoutBytes / (per_row > 0 ? per_row : 1) / kStepRows * kStepRows;
+        if (most < 8 * kStepRows) most = 8 * kStepRows;
+        if (p.rows > most) p.rows = most;
+    }
+    const int64_t padded = up_to(p.rows, kStepRows);
+    p.terms_bytes = lay_dy ? up_to(p.terms * padded * p.ld_terms * 2, 256) : 0;
+    p.kept_bytes = lay_x ? up_to(p.rows * p.ld_kept, 256) : 0;
+    p.slots_bytes = (int64_t)p.pairs * 4 * WgShape<256>::kSlotFloats * 4;
+    // chunks of rows for the bias: enough CTAs, each of 64 rows or more
+    const int64_t ctiles = (out_cols + 255) / 256;
+    int64_t chunks = (int64_t)sm_count * kBiasCtas / ctiles;
+    if (chunks > (rows + 63) / 64) chunks = (rows + 63) / 64;
+    if (chunks < 1) chunks = 1;
+    p.bias_chunk = (rows + chunks - 1) / chunks;
+    if (p.bias_chunk < 1) p.bias_chunk = 1;
+    p.bias_chunks = (int)((rows + p.bias_chunk - 1) / p.bias_chunk);
+    if (p.bias_chunks < 1) p.bias_chunks = 1;
+    p.bias_bytes = up_to((int64_t)p.bias_chunks * out_cols * 4, 256);
+    return p;
+}
+
+// cuTensorMapEncodeTiled, looked up once per process.
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) p = nullptr;
+        return (EncodeTiled)p;
+    }();
+    return f;
+}
+
+bool make_map(CUtensorMap* map, const void* p, bool bf16, int64_t cols, int64_t rows, int64_t ld_bytes, int box_cols)
+{
+    const EncodeTiled f = encode_tiled();
+    if (!f) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld_bytes};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)kStepRows}, steps[2] = {1, 1};
+    return f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), dims, strides, box, steps,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, bf16 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int BN>
+cudaError_t launch_product(const CUtensorMap& map_dy, const CUtensorMap& map_x, WgArgs a, cudaStream_t stream)
+{
+    a.tiles_m = (int)((a.out_cols + kTileM - 1) / kTileM);
+    a.tiles_n = (int)((a.cols + BN - 1) / BN);
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
+    if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
+    a.whole = (int)(tiles / a.pairs);
+    const int64_t left = tiles - (int64_t)a.whole * a.pairs;
+    a.rest = left * a.steps;
+    a.per = (a.rest + a.pairs - 1) / a.pairs;
+    if (a.per < kMinSteps) a.per = a.steps < kMinSteps ? a.steps : kMinSteps;
+    if (left == 0) a.per = a.steps;
+    const int64_t busy = a.whole ? a.pairs : (a.rest + a.per - 1) / a.per;
+    cudaError_t e = cudaFuncSetAttribute(k_wgrad<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, WgShape<BN>::kSmem);
+    if (e != cudaSuccess) return e;
     launch_begin("k_wgrad", stream);
-    const cudaError_t e = with_dtype(p.dtype, [&](auto elem) {
-        return launch_pdl(k_wgrad_any<decltype(elem)>, (int)ctas, kThreads, 0, stream, a);
-    });
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * busy));
+    cfg.blockDim = dim3(kWgThreads);
+    cfg.dynamicSmemBytes = WgShape<BN>::kSmem;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, k_wgrad<BN>, map_dy, map_x, a);
     launch_end(stream);
+    if (e != cudaSuccess || left == 0 || a.per % a.steps == 0) return e;  // no tile is split
+    launch_begin("k_wgrad_join", stream);
+    if (a.steps >= 8 * a.per)
+        e = launch_pdl(k_wgrad_join<BN, 8>, (int)(left * 256 * (BN / 8) / 32), kThreads, 0, stream, a);
+    else
+        e = launch_pdl(k_wgrad_join<BN, 1>, (int)(left * 256 * (BN / 8) / 256), kThreads, 0, stream, a);
+    launch_end(stream);
+    return e;
+}
+
+}  // namespace
+
+size_t ws_bytes_act8_wgrad(int64_t rows, int64_t cols, int64_t out_cols, int dtype, int sm_count)
+{
+    if (rows == 0 || out_cols == 0) return 0;
+    const Plan p = make_plan(rows, cols, out_cols, dtype, true, true, sm_count > 0 ? sm_count : 148);
+    // (with only one operand laid out a launch may take more rows, of at most kLayoutBytes)
+    int64_t lay = p.terms_bytes + p.kept_bytes;
+    for (int k = 1; k <= 2; ++k) {
+        const Plan q = make_plan(rows, cols, out_cols, dtype, k == 1, k == 2, sm_count > 0 ? sm_count : 148);
+        if (q.terms_bytes + q.kept_bytes > lay) lay = q.terms_bytes + q.kept_bytes;
+    }
+    return (size_t)(p.slots_bytes + p.bias_bytes + lay);
+}
+
+cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream)
+{
+    const bool acc = p.accumulate != 0;
+    cudaError_t e = cudaSuccess;
+    if (p.rows == 0) {
+        if (acc) return e;
+        const int64_t n = p.cols * p.out_cols, m = p.db ? p.out_cols : 0;
+        const int64_t want = (n + m + kThreads - 1) / kThreads, most = (int64_t)sm_count * 8;
+        launch_begin("k_wgrad_zero", stream);
+        e = launch_pdl(k_wgrad_zero, (int)(want < most ? want : most), kThreads, 0, stream, p.dw, n, p.db, m);
+        launch_end(stream);
+        return e;
+    }
+    const bool lay_dy = p.dtype != OGQ_BF16 || ((uintptr_t)p.dy & 15) || p.ld_dy % 8;
+    const bool lay_x = ((uintptr_t)p.codes & 15) || p.cols % 16;
+    const Plan plan = make_plan(p.rows, p.cols, p.out_cols, p.dtype, lay_dy, lay_x, sm_count);
+    char* ws = (char*)p.ws;
+    float* slots = (float*)ws;
+    float* bias_part = (float*)(ws + plan.slots_bytes);
+    uint16_t* terms = (uint16_t*)(ws + plan.slots_bytes + plan.bias_bytes);
+    int8_t* kept = (int8_t*)((char*)terms + plan.terms_bytes);
+
+    if (p.db) {
+        const int size = p.dtype == OGQ_F32 ? 4 : 2;
+        const bool vec = ((uintptr_t)p.dy & 15) == 0 && p.ld_dy * size % 16 == 0 && p.ld_dy % 8 == 0 && p.out_cols % 8 == 0;
+        WgBias b = {p.dy, p.ld_dy, p.rows, p.out_cols, plan.bias_chunk, bias_part, p.db, plan.bias_chunks, 0, acc};
+        b.ctiles = (int)((p.out_cols + (vec ? 255 : 31)) / (vec ? 256 : 32));
+        launch_begin("k_wgrad_bias", stream);
+        e = with_dtype(p.dtype, [&](auto elem) {
+            using E = decltype(elem);
+            return vec ? launch_pdl(k_wgrad_bias<E, 8>, b.ctiles * b.chunks, kThreads, 0, stream, b)
+                       : launch_pdl(k_wgrad_bias<E, 1>, b.ctiles * b.chunks, kThreads, 0, stream, b);
+        });
+        launch_end(stream);
+        if (e == cudaSuccess && b.chunks > 1) {
+            launch_begin("k_wgrad_bias_join", stream);
+            e = launch_pdl(k_wgrad_bias_join, (int)((p.out_cols + kThreads - 1) / kThreads), kThreads, 0, stream, b);
+            launch_end(stream);
+        }
+        if (e != cudaSuccess) return e;
+    }
+    if (p.cols == 0) return e;
+
+    WgArgs a = {};
+    a.dw = p.dw;
+    a.slots = slots;
+    a.cols = p.cols;
+    a.out_cols = p.out_cols;
+    a.groups = (int)act8_groups(p.cols);
+    a.pairs = plan.pairs;
+    a.wide = p.cols % 8 == 0 && ((uintptr_t)p.dw & 31) == 0;
+    const size_t size = p.dtype == OGQ_F32 ? 4 : 2;
+    for (int64_t t = 0; t < p.rows; t += plan.rows) {
+        const int64_t rows = p.rows - t < plan.rows ? p.rows - t : plan.rows;
+        const int64_t padded = up_to(rows, kStepRows);
+        const char* dy = (const char*)p.dy + t * p.ld_dy * size;
+        const int8_t* codes = p.codes + t * p.cols;
+        if (lay_dy || lay_x) {
+            WgLayout l = {dy, p.ld_dy, codes, lay_dy ? terms : nullptr, plan.ld_terms, lay_x ? kept : nullptr, plan.ld_kept, rows, padded, p.cols, p.out_cols};
+            const int64_t want = ((lay_dy ? padded * plan.ld_terms / 8 : 0) + (lay_x ? rows * plan.ld_kept / 16 : 0) + kThreads - 1) / kThreads;
+            const int ctas = (int)(want < (int64_t)sm_count * 8 ? want : (int64_t)sm_count * 8);
+            launch_begin("k_wgrad_layout", stream);
+            e = p.dtype == OGQ_F32 ? launch_pdl(k_wgrad_layout<float, 3>, ctas, kThreads, 0, stream, l)
+                : p.dtype == OGQ_F16 ? launch_pdl(k_wgrad_layout<__half, 2>, ctas, kThreads, 0, stream, l)
+                                     : launch_pdl(k_wgrad_layout<__nv_bfloat16, 1>, ctas, kThreads, 0, stream, l);
+            launch_end(stream);
+            if (e != cudaSuccess) return e;
+        }
+        CUtensorMap map_dy, map_x;
+        const bool narrow = p.cols <= 128;
+        const int terms_here = lay_dy ? plan.terms : 1;
+        if (!make_map(&map_dy, lay_dy ? (const void*)terms : dy, true, p.out_cols, lay_dy ? terms_here * padded : rows,
+                      (lay_dy ? plan.ld_terms : p.ld_dy) * 2, 64) ||
+            !make_map(&map_x, lay_x ? kept : codes, false, p.cols, rows, lay_x ? plan.ld_kept : p.cols, narrow ? 64 : 128))
+            return cudaErrorInvalidValue;
+        a.scales = p.scales + t * a.groups;
+        a.rows = rows;
+        a.steps_x = (int)(padded / kStepRows);
+        a.steps = terms_here * a.steps_x;
+        a.accumulate = acc || t > 0;
+        e = narrow ? launch_product<128>(map_dy, map_x, a, stream) : launch_product<256>(map_dy, map_x, a, stream);
+        if (e != cudaSuccess) return e;
+    }
     return e;
 }
 

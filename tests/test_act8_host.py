@@ -144,6 +144,9 @@ def test_wgrad_refuses():
     assert ogq.ogq_act8_wgrad_workspace_bytes(16, 32, 64, 5) == 0
     assert ogq.ogq_act8_wgrad_workspace_bytes(-1, 32, 64, 0) == 0
     assert ogq.ogq_act8_wgrad_workspace_bytes(100352, 64, 256, ogq.OGQ_BF16) > 0
+    for rows, cols, out in ((0, 32, 64), (16, 0, 64), (16, 32, 0), (0, 0, 0), (1, 1, 1)):
+        for d in (ogq.OGQ_F32, ogq.OGQ_F16, ogq.OGQ_BF16):
+            assert ogq.ogq_act8_wgrad_workspace_bytes(rows, cols, out, d) >= 256
 
 
 def test_group_norm_refuses():
