@@ -24,10 +24,11 @@ constexpr int kFlush = 8;                      // stages per running sum
 constexpr int kWgStages = 5;
 constexpr int kTileM = 256;                    // columns of dy per tile (both CTAs)
 constexpr int kABytes = 128 * kStepRows * 2;   // dy's tile of one CTA
-constexpr int kWgThreads = 512;                // a warpgroup for TMA, MMA and TMEM; one of converters; two that take sums out of TMEM
-// Registers a thread of the three kinds; the block starts with 512 * 128 = 65,536, which the split must not exceed.
-constexpr int kRegsControl = 40, kRegsConvert = 104, kRegsSums = 184;
-static_assert(128 * kRegsControl + 128 * kRegsConvert + 256 * kRegsSums <= kWgThreads * 128, "a warpgroup would wait for registers for ever");
+constexpr int kScaleBytes = kStepRows * 8;     // two words per row that hold the scale bytes of its (at most four) groups
+constexpr int kWgThreads = 640;                // a warpgroup for TMA, MMA, TMEM and units; two of converters; two that take sums out of TMEM
+// Registers a thread of the three kinds; the block starts with 640 * 96 = 61,440, which the split must not exceed.
+constexpr int kRegsStart = 96, kRegsControl = 48, kRegsConvert = 64, kRegsSums = 152;
+static_assert(128 * kRegsControl + 256 * kRegsConvert + 256 * kRegsSums <= kWgThreads * kRegsStart, "a warpgroup would wait for registers for ever");
 constexpr uint32_t kTmemColumns = 512;
 constexpr int kMinSteps = 8;                   // fewer steps than these are not split: a second launch costs more than they do
 
@@ -39,7 +40,8 @@ template <int BN> struct WgShape {
     static constexpr int kBBytes = kCols * kStepRows * 2;
     static constexpr int kRawBytes = kCols * kStepRows;
     static constexpr int kStageBytes = kABytes + kBBytes + kRawBytes;
-    static constexpr int kSmem = kWgStages * kStageBytes + 1024;  // + alignment to the swizzle's 1024 bytes
+    static_assert(kStageBytes % 1024 == 0, "the swizzle goes by the address");
+    static constexpr int kSmem = kWgStages * (kStageBytes + kScaleBytes) + 1024;  // + alignment to the swizzle's 1024 bytes
     static constexpr int kSlotFloats = 128 * BN;                  // a partial tile of one CTA
 };
 
@@ -115,30 +117,25 @@ __device__ __forceinline__ uint32_t wg_value2(uint32_t p, __nv_bfloat162 unit)
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// The scale bytes of this thread's rows of a step.
-template <int BN>
-__device__ __forceinline__ void wg_scales(const WgArgs& a, int step_x, int row, int group, uint32_t (&s)[WgShape<BN>::kRowsEach])
-{
-#pragma unroll
-    for (int j = 0; j < WgShape<BN>::kRowsEach; ++j) {
-        const int64_t t = (int64_t)step_x * kStepRows + row + WgShape<BN>::kRowsAtOnce * j;
-        s[j] = t < a.rows && group < a.groups ? (uint32_t)a.scales[t * a.groups + group] : 0u;
-    }
-}
-
-// This thread's rows, eight codes each: `raw` and `b` are this stage's, oct the thread's eight columns.  Eight lanes write the 128
+// This thread's rows, eight codes each, of the stage's codes, scales (from this thread's byte on) and place for the operand.  Eight lanes write the 128
 // bytes of a row of a swizzled block: no bank conflicts.
 template <int BN>
-__device__ __forceinline__ void wg_convert(uint32_t raw, uint32_t b, int row, int oct, const uint32_t (&s)[WgShape<BN>::kRowsEach])
+__device__ __forceinline__ void wg_convert(uint32_t raw, uint32_t scales, uint32_t b, int row, int oct)
 {
-    constexpr int kCols = WgShape<BN>::kCols;
+    constexpr int kCols = WgShape<BN>::kCols, kEach = WgShape<BN>::kRowsEach;
+    uint32_t c[kEach][2], u[kEach];  // all loads before the first store, which none could pass
 #pragma unroll
-    for (int j = 0; j < WgShape<BN>::kRowsEach; ++j) {
+    for (int j = 0; j < kEach; ++j) {
         const int t = row + WgShape<BN>::kRowsAtOnce * j;
-        uint32_t x, y;
-        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(raw + t * kCols + oct * 8));
-        const uint32_t u = s[j] << 7 | s[j] << 23;
-        const __nv_bfloat162 unit = *reinterpret_cast<const __nv_bfloat162*>(&u);
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(c[j][0]), "=r"(c[j][1]) : "r"(raw + t * kCols + oct * 8));
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(u[j]) : "r"(scales + t * 8));
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int t = row + WgShape<BN>::kRowsAtOnce * j;
+        const uint32_t x = c[j][0], y = c[j][1];
+        const uint32_t both = u[j] * 0x800080u;  // the byte is a bf16 number's exponent
+        const __nv_bfloat162 unit = *reinterpret_cast<const __nv_bfloat162*>(&both);
         const uint32_t v0 = wg_value2(__byte_perm(x, 0, 0x4140), unit), v1 = wg_value2(__byte_perm(x, 0, 0x4342), unit);
         const uint32_t v2 = wg_value2(__byte_perm(y, 0, 0x4140), unit), v3 = wg_value2(__byte_perm(y, 0, 0x4342), unit);
         const uint32_t at = b + (oct >> 3) * (kStepRows * 128) + t * 128 + (((oct ^ t) & 7) << 4);
@@ -185,7 +182,7 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
     const uint32_t rank = cluster_rank();
     const int pair = (int)(blockIdx.x >> 1);
     const uint32_t bar0 = smem_u32(bars);
-    // empty: the stage's MMAs are done (both CTAs).  raw: the codes are here.  dy (leader's): both CTAs' tiles of dy are here.
+    // empty: the stage's MMAs are done (both CTAs).  raw: the codes and their scales are here.  dy (leader's): both CTAs' tiles of dy are here.
     // ready (leader's): both CTAs' codes are converted.  sum: a running sum is complete (both).  taken (leader's): it has been read.
     const auto empty = [&](int s) { return bar0 + 8u * s; };
     const auto raw = [&](int s) { return bar0 + 8u * (kWgStages + s); };
@@ -196,11 +193,12 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
     const auto stage_a = [&](int s) { return base + s * S::kStageBytes; };
     const auto stage_b = [&](int s) { return base + s * S::kStageBytes + kABytes; };
     const auto stage_raw = [&](int s) { return base + s * S::kStageBytes + kABytes + S::kBBytes; };
+    const auto stage_scales = [&](int s) { return base + kWgStages * S::kStageBytes + s * kScaleBytes; };
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kWgStages; ++s) {
             mbar_init(empty(s), 1);
-            mbar_init(raw(s), 1);
+            mbar_init(raw(s), 33);  // TMA's and those of the lanes that copy the scales
             mbar_init(dyb(s), 1);
             mbar_init(ready(s), 8);
         }
@@ -275,41 +273,62 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
                 }
             }
         }
-    } else if (warp < 8) {  // converters
+        else if (warp == 3) {  // scales: the aligned words around each row's bytes, never past the end
+            WgWork w(a, pair);
+            int s = 0;
+            uint32_t phase = 1;
+            bool ok = true;
+            const int64_t all = a.rows * a.groups;
+            while (ok && w.next(a, pair)) {
+                int m, n;
+                wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
+                const int first = (n * BN + (int)rank * S::kCols) / kAct8Group;
+                for (int k = w.k0; k < w.k1; ++k) {
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(empty(s), phase, &failed)))) break;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = lane + (r >> 1) * 32;
+                        const int64_t t = (int64_t)(k % a.steps_x) * kStepRows + row;
+                        const int64_t at = ((t * a.groups + first) & ~(int64_t)3) + (r & 1) * 4;
+                        const int64_t left = t < a.rows ? all - at : 0;
+                        copy4_async(stage_scales(s) + row * 8 + (r & 1) * 4, a.scales + (left > 0 ? at : 0), left >= 4 ? 4 : left > 0 ? (int)left : 0);
+                    }
+                    copies_arrive(raw(s));
+                    if (++s == kWgStages) { s = 0; phase ^= 1; }
+                }
+            }
+        }
+    } else if (warp < 12) {  // converters: every other stage
         fewer_registers<kRegsConvert>();
-        const int id = threadIdx.x - 128;
+        const int which = (warp - 4) >> 2, id = threadIdx.x & 127;
         const int oct = id % S::kOcts, row = id / S::kOcts;
         WgWork w(a, pair);
-        int s = 0;
+        int s = which;
         uint32_t phase = 0;
         bool ok = true;
-        const auto step = [&](const uint32_t (&u)[S::kRowsEach]) {
-            if (!(ok = __all_sync(0xffffffffu, mbar_wait(raw(s), phase, &failed)))) return;
-            wg_convert<BN>(stage_raw(s), stage_b(s), row, oct, u);
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(map_to(ready(s), 0));
-            if (++s == kWgStages) { s = 0; phase ^= 1; }
-        };
+        int turn = which;  // steps until this warpgroup's next one
         while (ok && w.next(a, pair)) {
             int m, n;
             wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
-            const int group = (n * BN + (int)rank * S::kCols) / kAct8Group + oct / 4;
-            uint32_t u[S::kRowsEach], v[S::kRowsEach];  // scales two steps ahead: they come from L2 or memory
-            wg_scales<BN>(a, w.k0 % a.steps_x, row, group, u);
-            if (w.k0 + 1 < w.k1) wg_scales<BN>(a, (w.k0 + 1) % a.steps_x, row, group, v);
-            for (int k = w.k0; ok && k < w.k1; k += 2) {
-                step(u);
-                if (k + 2 < w.k1) wg_scales<BN>(a, (k + 2) % a.steps_x, row, group, u);
-                if (!ok || k + 1 >= w.k1) break;
-                step(v);
-                if (k + 3 < w.k1) wg_scales<BN>(a, (k + 3) % a.steps_x, row, group, v);
+            // a row's bytes begin at this byte of its first word; eight rows on it is the same one
+            const int first = (n * BN + (int)rank * S::kCols) / kAct8Group;
+            const int byte = ((row * a.groups + first) & 3) + oct / 4;
+            int k = w.k0 + turn;
+            for (; k < w.k1; k += 2) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(raw(s), phase, &failed)))) break;
+                wg_convert<BN>(stage_raw(s), stage_scales(s) + byte, stage_b(s), row, oct);
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to(ready(s), 0));
+                s += 2;
+                if (s >= kWgStages) { s -= kWgStages; phase ^= 1; }
             }
+            turn = k - w.k1;
         }
     } else {  // sums out of TMEM, and out
         more_registers<kRegsSums>();
         constexpr int kHalf = BN / 2;
-        const int quarter = warp & 3, half = (warp - 8) >> 2;
+        const int quarter = warp & 3, half = (warp - 12) >> 2;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         WgWork w(a, pair);
         int d = 0;
@@ -409,13 +428,14 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_join(const __grid_constant__
 // ---------------------------------------------------------------------------
 // Operands that TMA cannot read as they are (fp16, fp32, rows off 16-byte boundaries) are laid out in the scratch first:
 // dy as bf16 terms stacked along t, each of `padded` rows (a multiple of 64, zeros behind the last), and the codes with rows of
-// a multiple of 16 bytes.
+// a multiple of 16 bytes; scales off 4-byte boundaries are copied too.
 // ---------------------------------------------------------------------------
 struct WgLayout {
     const void* dy; int64_t ld_dy;
     const int8_t* codes;
     uint16_t* terms; int64_t ld_terms;   // null: dy is read as it is
     int8_t* kept; int64_t ld_kept;       // null: the codes are
+    const uint8_t* scales; uint8_t* scales_to; int64_t n_scales;  // scales_to null: the scales are
     int64_t rows, padded, cols, out_cols;
 };
 
@@ -465,6 +485,8 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_layout(const __grid_constant
             *reinterpret_cast<uint4*>(a.kept + t * a.ld_kept + c) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
+    if (a.scales_to)
+        for (int64_t i = id; i < a.n_scales; i += stride) a.scales_to[i] = a.scales[i];
 }
 
 // ---------------------------------------------------------------------------
@@ -548,27 +570,27 @@ int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 int terms_of(int dtype) { return dtype == OGQ_F32 ? 3 : dtype == OGQ_F16 ? 2 : 1; }
 
 struct Plan {
-    bool lay_dy, lay_x;
+    bool lay_dy, lay_x, lay_s;
     int terms, pairs;
     int64_t ld_terms, ld_kept, rows;  // rows per launch
-    int64_t slots_bytes, bias_bytes, terms_bytes, kept_bytes;
+    int64_t slots_bytes, bias_bytes, terms_bytes, kept_bytes, scales_bytes;
     int64_t bias_chunk;
     int bias_chunks;
 };
 
-// Laid out or not is decided by the call's addresses; the scratch is sized for the worse.
-Plan make_plan(int64_t rows, int64_t cols, int64_t out_cols, int dtype, bool lay_dy, bool lay_x, int sm_count)
+Plan make_plan(int64_t rows, int64_t cols, int64_t out_cols, int dtype, bool lay_dy, bool lay_x, bool lay_s, int sm_count)
 {
     Plan p = {};
     p.lay_dy = lay_dy;
     p.lay_x = lay_x;
+    p.lay_s = lay_s;
     p.terms = terms_of(dtype);
     p.pairs = sm_count / 2;
     p.ld_terms = up_to(out_cols, 8);
     p.ld_kept = up_to(cols, 16);
     p.rows = rows;
-    if (lay_dy || lay_x) {
-        const int64_t per_row = (lay_dy ? p.terms * p.ld_terms * 2 : 0) + (lay_x ? p.ld_kept : 0);
+    if (lay_dy || lay_x || lay_s) {
+        const int64_t per_row = (lay_dy ? p.terms * p.ld_terms * 2 : 0) + (lay_x ? p.ld_kept : 0) + (lay_s ? act8_groups(cols) : 0);
         int64_t most = kLayoutBytes / (per_row > 0 ? per_row : 1) / kStepRows * kStepRows;
         if (most < 8 * kStepRows) most = 8 * kStepRows;
         if (p.rows > most) p.rows = most;
@@ -576,6 +598,7 @@ Plan make_plan(int64_t rows, int64_t cols, int64_t out_cols, int dtype, bool lay
     const int64_t padded = up_to(p.rows, kStepRows);
     p.terms_bytes = lay_dy ? up_to(p.terms * padded * p.ld_terms * 2, 256) : 0;
     p.kept_bytes = lay_x ? up_to(p.rows * p.ld_kept, 256) : 0;
+    p.scales_bytes = lay_s ? up_to(p.rows * act8_groups(cols), 256) : 0;
     p.slots_bytes = (int64_t)p.pairs * 4 * WgShape<256>::kSlotFloats * 4;
     // chunks of rows for the bias: enough CTAs, each of 64 rows or more
     const int64_t ctiles = (out_cols + 255) / 256;
@@ -659,12 +682,13 @@ cudaError_t launch_product(const CUtensorMap& map_dy, const CUtensorMap& map_x, 
 size_t ws_bytes_act8_wgrad(int64_t rows, int64_t cols, int64_t out_cols, int dtype, int sm_count)
 {
     if (rows == 0 || out_cols == 0) return 0;
-    const Plan p = make_plan(rows, cols, out_cols, dtype, true, true, sm_count > 0 ? sm_count : 148);
-    // (with only one operand laid out a launch may take more rows, of at most kLayoutBytes)
-    int64_t lay = p.terms_bytes + p.kept_bytes;
-    for (int k = 1; k <= 2; ++k) {
-        const Plan q = make_plan(rows, cols, out_cols, dtype, k == 1, k == 2, sm_count > 0 ? sm_count : 148);
-        if (q.terms_bytes + q.kept_bytes > lay) lay = q.terms_bytes + q.kept_bytes;
+    // Which operands are laid out depends on the call's addresses (a launch takes more rows when fewer are): room for every choice.
+    Plan p = {};
+    int64_t lay = 0;
+    for (int k = 0; k < 8; ++k) {
+        p = make_plan(rows, cols, out_cols, dtype, (k & 1) != 0, (k & 2) != 0, (k & 4) != 0, sm_count > 0 ? sm_count : 148);
+        const int64_t b = p.terms_bytes + p.kept_bytes + p.scales_bytes;
+        if (b > lay) lay = b;
     }
     return (size_t)(p.slots_bytes + p.bias_bytes + lay);
 }
@@ -684,12 +708,14 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
     }
     const bool lay_dy = p.dtype != OGQ_BF16 || ((uintptr_t)p.dy & 15) || p.ld_dy % 8;
     const bool lay_x = ((uintptr_t)p.codes & 15) || p.cols % 16;
-    const Plan plan = make_plan(p.rows, p.cols, p.out_cols, p.dtype, lay_dy, lay_x, sm_count);
+    const bool lay_s = ((uintptr_t)p.scales & 3) != 0;
+    const Plan plan = make_plan(p.rows, p.cols, p.out_cols, p.dtype, lay_dy, lay_x, lay_s, sm_count);
     char* ws = (char*)p.ws;
     float* slots = (float*)ws;
     float* bias_part = (float*)(ws + plan.slots_bytes);
     uint16_t* terms = (uint16_t*)(ws + plan.slots_bytes + plan.bias_bytes);
     int8_t* kept = (int8_t*)((char*)terms + plan.terms_bytes);
+    uint8_t* scales_to = (uint8_t*)kept + plan.kept_bytes;
 
     if (p.db) {
         const int size = p.dtype == OGQ_F32 ? 4 : 2;
@@ -726,9 +752,11 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
         const int64_t padded = up_to(rows, kStepRows);
         const char* dy = (const char*)p.dy + t * p.ld_dy * size;
         const int8_t* codes = p.codes + t * p.cols;
-        if (lay_dy || lay_x) {
-            WgLayout l = {dy, p.ld_dy, codes, lay_dy ? terms : nullptr, plan.ld_terms, lay_x ? kept : nullptr, plan.ld_kept, rows, padded, p.cols, p.out_cols};
-            const int64_t want = ((lay_dy ? padded * plan.ld_terms / 8 : 0) + (lay_x ? rows * plan.ld_kept / 16 : 0) + kThreads - 1) / kThreads;
+        const uint8_t* scales = p.scales + t * a.groups;
+        if (lay_dy || lay_x || lay_s) {
+            WgLayout l = {dy, p.ld_dy, codes, lay_dy ? terms : nullptr, plan.ld_terms, lay_x ? kept : nullptr, plan.ld_kept,
+                          scales, lay_s ? scales_to : nullptr, rows * a.groups, rows, padded, p.cols, p.out_cols};
+            const int64_t want = ((lay_dy ? padded * plan.ld_terms / 8 : 0) + (lay_x ? rows * plan.ld_kept / 16 : 0) + (lay_s ? rows * a.groups : 0) + kThreads - 1) / kThreads;
             const int ctas = (int)(want < (int64_t)sm_count * 8 ? want : (int64_t)sm_count * 8);
             launch_begin("k_wgrad_layout", stream);
             e = p.dtype == OGQ_F32 ? launch_pdl(k_wgrad_layout<float, 3>, ctas, kThreads, 0, stream, l)
@@ -744,7 +772,7 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
                       (lay_dy ? plan.ld_terms : p.ld_dy) * 2, 64) ||
             !make_map(&map_x, lay_x ? kept : codes, false, p.cols, rows, lay_x ? plan.ld_kept : p.cols, narrow ? 64 : 128))
             return cudaErrorInvalidValue;
-        a.scales = p.scales + t * a.groups;
+        a.scales = lay_s ? scales_to : scales;
         a.rows = rows;
         a.steps_x = (int)(padded / kStepRows);
         a.steps = terms_here * a.steps_x;
