@@ -21,10 +21,10 @@ namespace ogq {
 
 constexpr int kStepRows = 64;                  // rows of t per stage
 constexpr int kFlush = 8;                      // stages per running sum
-constexpr int kWgStages = 5;
+constexpr int kOperands = 3;                   // converted tiles of x^: one being written by each warpgroup, one being multiplied
 constexpr int kTileM = 256;                    // columns of dy per tile (both CTAs)
 constexpr int kABytes = 128 * kStepRows * 2;   // dy's tile of one CTA
-constexpr int kScaleBytes = kStepRows * 8;     // two words per row that hold the scale bytes of its (at most four) groups
+constexpr int kScaleBytes = kStepRows * 16;    // scales around those of a tile's (at most four) groups: 16 bytes a row by TMA, or two words
 constexpr int kWgThreads = 640;                // a warpgroup for TMA, MMA, TMEM and units; two of converters; two that take sums out of TMEM
 // Registers a thread of the three kinds; the block starts with 640 * 96 = 61,440, which the split must not exceed.
 constexpr int kRegsStart = 96, kRegsControl = 48, kRegsConvert = 64, kRegsSums = 152;
@@ -39,9 +39,12 @@ template <int BN> struct WgShape {
     static constexpr int kRowsEach = kStepRows / kRowsAtOnce;
     static constexpr int kBBytes = kCols * kStepRows * 2;
     static constexpr int kRawBytes = kCols * kStepRows;
-    static constexpr int kStageBytes = kABytes + kBBytes + kRawBytes;
-    static_assert(kStageBytes % 1024 == 0, "the swizzle goes by the address");
-    static constexpr int kSmem = kWgStages * (kStageBytes + kScaleBytes) + 1024;  // + alignment to the swizzle's 1024 bytes
+    // Loads under way: a stage is in use from the request (2,200 cycles until the data is there when it comes from memory) until its
+    // product is done, some 3,600 cycles against 510 for the product itself; the converted tiles are needed for less than half of that.
+    static constexpr int kStages = BN == 256 ? 7 : 8;
+    static constexpr int kSmem = kStages * (kABytes + kRawBytes + kScaleBytes) + kOperands * kBBytes + 1024;  // + alignment to the swizzle's 1024 bytes
+    static_assert(kABytes % 1024 == 0 && kBBytes % 1024 == 0, "the swizzle goes by the address");
+    static_assert(kSmem <= 226 * 1024, "shared memory");
     static constexpr int kSlotFloats = 128 * BN;                  // a partial tile of one CTA
 };
 
@@ -61,6 +64,7 @@ struct WgArgs {
     int64_t per;        // of them per pair
     bool accumulate;
     bool wide;          // 32-byte stores
+    bool tma_scales;    // a multiple of 16 groups: TMA copies the scales
 };
 
 // The pieces of work of one pair: (tile, steps [k0, k1)), the same sequence in every role.
@@ -120,7 +124,7 @@ __device__ __forceinline__ uint32_t wg_value2(uint32_t p, __nv_bfloat162 unit)
 // This thread's rows, eight codes each, of the stage's codes, scales (from this thread's byte on) and place for the operand.  Eight lanes write the 128
 // bytes of a row of a swizzled block: no bank conflicts.
 template <int BN>
-__device__ __forceinline__ void wg_convert(uint32_t raw, uint32_t scales, uint32_t b, int row, int oct)
+__device__ __forceinline__ void wg_convert(uint32_t raw, uint32_t scales, int pitch, uint32_t b, int row, int oct)
 {
     constexpr int kCols = WgShape<BN>::kCols, kEach = WgShape<BN>::kRowsEach;
     uint32_t c[kEach][2], u[kEach];  // all loads before the first store, which none could pass
@@ -128,7 +132,7 @@ __device__ __forceinline__ void wg_convert(uint32_t raw, uint32_t scales, uint32
     for (int j = 0; j < kEach; ++j) {
         const int t = row + WgShape<BN>::kRowsAtOnce * j;
         asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(c[j][0]), "=r"(c[j][1]) : "r"(raw + t * kCols + oct * 8));
-        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(u[j]) : "r"(scales + t * 8));
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(u[j]) : "r"(scales + t * pitch));
     }
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
@@ -170,11 +174,13 @@ __device__ __forceinline__ void wg_store8(const WgArgs& a, int64_t o, int64_t i,
 
 template <int BN>
 __global__ void __launch_bounds__(kWgThreads, 1) __cluster_dims__(2, 1, 1)
-k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ WgArgs a)
+k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x,
+        const __grid_constant__ CUtensorMap map_scales, const __grid_constant__ WgArgs a)
 {
     using S = WgShape<BN>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[4 * kWgStages + 4];
+    constexpr int kStages = S::kStages;
+    __shared__ uint64_t bars[4 * kStages + kOperands + 4];
     __shared__ uint32_t tmem_base;
     __shared__ volatile int failed;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -182,26 +188,30 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
     const uint32_t rank = cluster_rank();
     const int pair = (int)(blockIdx.x >> 1);
     const uint32_t bar0 = smem_u32(bars);
-    // empty: the stage's MMAs are done (both CTAs).  raw: the codes and their scales are here.  dy (leader's): both CTAs' tiles of dy are here.
-    // ready (leader's): both CTAs' codes are converted.  sum: a running sum is complete (both).  taken (leader's): it has been read.
-    const auto empty = [&](int s) { return bar0 + 8u * s; };
-    const auto raw = [&](int s) { return bar0 + 8u * (kWgStages + s); };
-    const auto dyb = [&](int s) { return bar0 + 8u * (2 * kWgStages + s); };
-    const auto ready = [&](int s) { return bar0 + 8u * (3 * kWgStages + s); };
-    const auto sum = [&](int d) { return bar0 + 8u * (4 * kWgStages + d); };
-    const auto taken = [&](int d) { return bar0 + 8u * (4 * kWgStages + 2 + d); };
-    const auto stage_a = [&](int s) { return base + s * S::kStageBytes; };
-    const auto stage_b = [&](int s) { return base + s * S::kStageBytes + kABytes; };
-    const auto stage_raw = [&](int s) { return base + s * S::kStageBytes + kABytes + S::kBBytes; };
-    const auto stage_scales = [&](int s) { return base + kWgStages * S::kStageBytes + s * kScaleBytes; };
+    // dy_here (leader's): both CTAs' tiles of dy are here.  raw_here: codes and scales are here; raw_free: they are converted.
+    // op_here (leader's): both CTAs' converted tiles are.  done (both): the step is multiplied, its tile of dy and its converted
+    // tile are free (one barrier for both: a commit holds the issuing thread up for 150 cycles and more).
+    // sum (both): a running sum is complete; taken (leader's): both CTAs have read it.
+    const auto dy_here = [&](int s) { return bar0 + 8u * s; };
+    const auto done = [&](int s) { return bar0 + 8u * (kStages + s); };
+    const auto raw_here = [&](int s) { return bar0 + 8u * (2 * kStages + s); };
+    const auto raw_free = [&](int s) { return bar0 + 8u * (3 * kStages + s); };
+    const auto op_here = [&](int b) { return bar0 + 8u * (4 * kStages + b); };
+    const auto sum = [&](int d) { return bar0 + 8u * (4 * kStages + kOperands + d); };
+    const auto taken = [&](int d) { return bar0 + 8u * (4 * kStages + kOperands + 2 + d); };
+    const auto stage_a = [&](int s) { return base + s * kABytes; };
+    const auto operand_b = [&](int b) { return base + kStages * kABytes + b * S::kBBytes; };
+    const auto stage_raw = [&](int s) { return base + kStages * kABytes + kOperands * S::kBBytes + s * S::kRawBytes; };
+    const auto stage_scales = [&](int s) { return base + kStages * (kABytes + S::kRawBytes) + kOperands * S::kBBytes + s * kScaleBytes; };
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kWgStages; ++s) {
-            mbar_init(empty(s), 1);
-            mbar_init(raw(s), 33);  // TMA's and those of the lanes that copy the scales
-            mbar_init(dyb(s), 1);
-            mbar_init(ready(s), 8);
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(dy_here(s), 1);
+            mbar_init(done(s), 1);
+            mbar_init(raw_here(s), a.tma_scales ? 1 : 33);  // TMA's, and those of the lanes that copy the scales
+            mbar_init(raw_free(s), 4);
         }
+        for (int b = 0; b < kOperands; ++b) mbar_init(op_here(b), 8);
         for (int d = 0; d < 2; ++d) {
             mbar_init(sum(d), 1);
             mbar_init(taken(d), 16);
@@ -221,35 +231,52 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
 
     if (warp < 4) {
         fewer_registers<kRegsControl>();
-        if (warp == 0 && lane == 0) {  // TMA
+        if (warp == 0 && lane == 0) {  // dy, by TMA
             WgWork w(a, pair);
             int s = 0;
-            uint32_t phase = 1;  // the first pass over the stages finds them empty
+            uint32_t phase = 1;  // the first pass over the stages finds them free
+            bool ok = true;
+            const uint32_t here = map_to(dy_here(0), 0);
+            while (ok && w.next(a, pair)) {
+                int m, n;
+                wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
+                const int o = m * kTileM + (int)rank * 128;
+                for (int k = w.k0; k < w.k1; ++k) {
+                    if (!(ok = mbar_wait(done(s), phase, &failed))) break;
+                    if (rank == 0) mbar_expect(dy_here(s), 2 * kABytes);
+                    tma_load_pair(stage_a(s), &map_dy, o, k * kStepRows, here + 8 * s);
+                    tma_load_pair(stage_a(s) + kABytes / 2, &map_dy, o + 64, k * kStepRows, here + 8 * s);
+                    if (++s == kStages) { s = 0; phase ^= 1; }
+                }
+            }
+            // Until the last copies have landed: a stage is free again when its MMAs, and so its copies, are done.
+            for (int k = 0; k < kStages; ++k) {
+                if (!mbar_wait(done(s), phase, &failed)) break;
+                if (++s == kStages) { s = 0; phase ^= 1; }
+            }
+        } else if (warp == 2 && lane == 0) {  // codes, by TMA (a thread for both kinds took 750 cycles a step to issue them)
+            WgWork w(a, pair);
+            int s = 0;
+            uint32_t phase = 1;
             bool ok = true;
             while (ok && w.next(a, pair)) {
                 int m, n;
                 wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
-                const int o = m * kTileM + (int)rank * 128, i = n * BN + (int)rank * S::kCols;
+                const int i = n * BN + (int)rank * S::kCols;
+                int x = w.k0 % a.steps_x;
                 for (int k = w.k0; k < w.k1; ++k) {
-                    if (!(ok = mbar_wait(empty(s), phase, &failed))) break;
-                    const uint32_t dy_bar = map_to(dyb(s), 0);
-                    if (rank == 0) mbar_expect(dyb(s), 2 * kABytes);
-                    mbar_expect(raw(s), S::kRawBytes);
-                    tma_load_pair(stage_raw(s), &map_x, i, k % a.steps_x * kStepRows, raw(s));
-                    tma_load_pair(stage_a(s), &map_dy, o, k * kStepRows, dy_bar);
-                    tma_load_pair(stage_a(s) + kABytes / 2, &map_dy, o + 64, k * kStepRows, dy_bar);
-                    if (++s == kWgStages) { s = 0; phase ^= 1; }
+                    if (!(ok = mbar_wait(raw_free(s), phase, &failed))) break;
+                    mbar_expect(raw_here(s), S::kRawBytes + (a.tma_scales ? kScaleBytes : 0));
+                    tma_load_pair(stage_raw(s), &map_x, i, x * kStepRows, raw_here(s));
+                    if (a.tma_scales) tma_load_pair(stage_scales(s), &map_scales, i / kAct8Group & ~15, x * kStepRows, raw_here(s));
+                    if (++x == a.steps_x) x = 0;
+                    if (++s == kStages) { s = 0; phase ^= 1; }
                 }
-            }
-            // Until the last copies have landed: a stage is free again when its MMAs, and so its copies, are done.
-            for (int k = 0; k < kWgStages; ++k) {
-                if (!mbar_wait(empty(s), phase, &failed)) break;
-                if (++s == kWgStages) { s = 0; phase ^= 1; }
             }
         } else if (warp == 1 && lane == 0 && rank == 0) {  // MMA of both CTAs
             WgWork w(a, pair);
-            int s = 0, d = 0;
-            uint32_t phase = 0, dphase = 1;
+            int s = 0, b = 0, d = 0;
+            uint32_t phase = 0, bphase = 0, dphase = 1;
             bool ok = true;
             constexpr uint32_t instruction = instruction_bf16(kTileM, BN);
             while (ok && w.next(a, pair)) {
@@ -258,14 +285,15 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
                     if (!(ok = mbar_wait(taken(d), dphase, &failed))) break;
                     tcgen05_fence_after();
                     for (int q = k; q < last; ++q) {
-                        if (!(ok = mbar_wait(dyb(s), phase, &failed) && mbar_wait(ready(s), phase, &failed))) break;
+                        if (!(ok = mbar_wait(dy_here(s), phase, &failed) && mbar_wait(op_here(b), bphase, &failed))) break;
                         tcgen05_fence_after();
-                        const uint64_t da = tile_descriptor(stage_a(s), kStepRows * 128), db = tile_descriptor(stage_b(s), kStepRows * 128);
+                        const uint64_t da = tile_descriptor(stage_a(s), kStepRows * 128), db = tile_descriptor(operand_b(b), kStepRows * 128);
 #pragma unroll
                         for (int j = 0; j < kStepRows / 16; ++j)  // 16 rows are 2048 bytes on
                             mma_bf16_pair(tmem + d * BN, da + j * (2048 >> 4), db + j * (2048 >> 4), instruction, q > k || j > 0);
-                        mma_commit_pair(empty(s));
-                        if (++s == kWgStages) { s = 0; phase ^= 1; }
+                        mma_commit_pair(done(s));
+                        if (++b == kOperands) { b = 0; bphase ^= 1; }
+                        if (++s == kStages) { s = 0; phase ^= 1; }
                     }
                     if (!ok) break;
                     mma_commit_pair(sum(d));
@@ -273,7 +301,7 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
                 }
             }
         }
-        else if (warp == 3) {  // scales: the aligned words around each row's bytes, never past the end
+        else if (warp == 3 && !a.tma_scales) {  // scales: the aligned words around each row's bytes, never past the end
             WgWork w(a, pair);
             int s = 0;
             uint32_t phase = 1;
@@ -283,18 +311,20 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
                 int m, n;
                 wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
                 const int first = (n * BN + (int)rank * S::kCols) / kAct8Group;
+                int x = w.k0 % a.steps_x;
                 for (int k = w.k0; k < w.k1; ++k) {
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(empty(s), phase, &failed)))) break;
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(raw_free(s), phase, &failed)))) break;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int row = lane + (r >> 1) * 32;
-                        const int64_t t = (int64_t)(k % a.steps_x) * kStepRows + row;
+                        const int64_t t = (int64_t)x * kStepRows + row;
                         const int64_t at = ((t * a.groups + first) & ~(int64_t)3) + (r & 1) * 4;
                         const int64_t left = t < a.rows ? all - at : 0;
                         copy4_async(stage_scales(s) + row * 8 + (r & 1) * 4, a.scales + (left > 0 ? at : 0), left >= 4 ? 4 : left > 0 ? (int)left : 0);
                     }
-                    copies_arrive(raw(s));
-                    if (++s == kWgStages) { s = 0; phase ^= 1; }
+                    copies_arrive(raw_here(s));
+                    if (++x == a.steps_x) x = 0;
+                    if (++s == kStages) { s = 0; phase ^= 1; }
                 }
             }
         }
@@ -303,25 +333,33 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
         const int which = (warp - 4) >> 2, id = threadIdx.x & 127;
         const int oct = id % S::kOcts, row = id / S::kOcts;
         WgWork w(a, pair);
-        int s = which;
-        uint32_t phase = 0;
+        // the operand's place is free when the step kOperands before this one is done (none for the first kOperands)
+        int s = which, b = which, before = which + kStages - kOperands;
+        uint32_t phase = 0, before_phase = 1;
         bool ok = true;
         int turn = which;  // steps until this warpgroup's next one
         while (ok && w.next(a, pair)) {
             int m, n;
             wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
-            // a row's bytes begin at this byte of its first word; eight rows on it is the same one
+            // this thread's byte of a row's; of words, the first holds the row's at a place that is the same eight rows on
             const int first = (n * BN + (int)rank * S::kCols) / kAct8Group;
-            const int byte = ((row * a.groups + first) & 3) + oct / 4;
+            const int byte = (a.tma_scales ? first & 15 : (row * a.groups + first) & 3) + oct / 4;
             int k = w.k0 + turn;
             for (; k < w.k1; k += 2) {
-                if (!(ok = __all_sync(0xffffffffu, mbar_wait(raw(s), phase, &failed)))) break;
-                wg_convert<BN>(stage_raw(s), stage_scales(s) + byte, stage_b(s), row, oct);
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(raw_here(s), phase, &failed) && mbar_wait(done(before), before_phase, &failed)))) break;
+                wg_convert<BN>(stage_raw(s), stage_scales(s) + byte, a.tma_scales ? 16 : 8, operand_b(b), row, oct);
                 fence_async_shared();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(map_to(ready(s), 0));
+                if (lane == 0) {
+                    mbar_arrive_cluster(map_to(op_here(b), 0));
+                    mbar_arrive(raw_free(s));
+                }
                 s += 2;
-                if (s >= kWgStages) { s -= kWgStages; phase ^= 1; }
+                if (s >= kStages) { s -= kStages; phase ^= 1; }
+                before += 2;
+                if (before >= kStages) { before -= kStages; before_phase ^= 1; }
+                b += 2;
+                if (b >= kOperands) b -= kOperands;
             }
             turn = k - w.k1;
         }
@@ -627,6 +665,7 @@ EncodeTiled encode_tiled()
     return f;
 }
 
+// A matrix of bf16 (swizzled boxes) or bytes.
 bool make_map(CUtensorMap* map, const void* p, bool bf16, int64_t cols, int64_t rows, int64_t ld_bytes, int box_cols)
 {
     const EncodeTiled f = encode_tiled();
@@ -639,7 +678,7 @@ bool make_map(CUtensorMap* map, const void* p, bool bf16, int64_t cols, int64_t 
 }
 
 template <int BN>
-cudaError_t launch_product(const CUtensorMap& map_dy, const CUtensorMap& map_x, WgArgs a, cudaStream_t stream)
+cudaError_t launch_product(const CUtensorMap& map_dy, const CUtensorMap& map_x, const CUtensorMap& map_scales, WgArgs a, cudaStream_t stream)
 {
     a.tiles_m = (int)((a.out_cols + kTileM - 1) / kTileM);
     a.tiles_n = (int)((a.cols + BN - 1) / BN);
@@ -665,7 +704,7 @@ cudaError_t launch_product(const CUtensorMap& map_dy, const CUtensorMap& map_x, 
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, k_wgrad<BN>, map_dy, map_x, a);
+    e = cudaLaunchKernelEx(&cfg, k_wgrad<BN>, map_dy, map_x, map_scales, a);
     launch_end(stream);
     if (e != cudaSuccess || left == 0 || a.per % a.steps == 0) return e;  // no tile is split
     launch_begin("k_wgrad_join", stream);
@@ -765,19 +804,24 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
             launch_end(stream);
             if (e != cudaSuccess) return e;
         }
-        CUtensorMap map_dy, map_x;
+        CUtensorMap map_dy, map_x, map_scales;
         const bool narrow = p.cols <= 128;
         const int terms_here = lay_dy ? plan.terms : 1;
         if (!make_map(&map_dy, lay_dy ? (const void*)terms : dy, true, p.out_cols, lay_dy ? terms_here * padded : rows,
                       (lay_dy ? plan.ld_terms : p.ld_dy) * 2, 64) ||
             !make_map(&map_x, lay_x ? kept : codes, false, p.cols, rows, lay_x ? plan.ld_kept : p.cols, narrow ? 64 : 128))
             return cudaErrorInvalidValue;
+        // Scales a row apart are 64 requests a step either way, but copied by a warp they also take 128 cycles a step from the shared
+        // memory pipe, which is what bounds the loop (16,384 x 4096 x 4096: 504 -> 404 us with TMA).
         a.scales = lay_s ? scales_to : scales;
+        a.tma_scales = a.groups % 16 == 0 && ((uintptr_t)a.scales & 15) == 0;
+        if (!a.tma_scales) map_scales = map_x;  // not used
+        else if (!make_map(&map_scales, a.scales, false, a.groups, rows, a.groups, 16)) return cudaErrorInvalidValue;
         a.rows = rows;
         a.steps_x = (int)(padded / kStepRows);
         a.steps = terms_here * a.steps_x;
         a.accumulate = acc || t > 0;
-        e = narrow ? launch_product<128>(map_dy, map_x, a, stream) : launch_product<256>(map_dy, map_x, a, stream);
+        e = narrow ? launch_product<128>(map_dy, map_x, map_scales, a, stream) : launch_product<256>(map_dy, map_x, map_scales, a, stream);
         if (e != cudaSuccess) return e;
     }
     return e;
