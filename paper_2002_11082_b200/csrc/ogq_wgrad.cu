@@ -2,15 +2,15 @@
 //   dW[o][i] = sum_t dy[t][o] x^[t][i]:  a product whose summed index t is the row of both operands.  x^ = code * 2^e is a bf16
 // number, so nothing is lost by multiplying in bf16: dy in bf16 goes to the tensor cores as it is, dy in fp16 and fp32 as the sum
 // of two and three bf16 terms (8 + 3 and 8 + 8 + 8 bits), stacked along t.
-//   A pair of CTAs works on a tile of 256 x BN weights, 64 rows of t at a time: TMA brings dy's tile (swizzled, the operand as it lies
+//   A pair of CTAs works on a tile of 256 x BN weights, 128 rows of t at a time: TMA brings dy's tile (swizzled, the operand as it lies
 // in memory) and the codes; four warps turn the codes into bf16 in shared memory (5 instructions for two values); one thread issues
 // the MMAs of both CTAs.  Pairs: each SM holds half of x^'s tile, so every code is converted once for 256 columns of dy, and both
 // operands cost half the shared memory traffic of single CTAs.
 //   The tensor cores cut, not round, what they add to a running sum, which drifts by 2^-24 a step: a sum over 16,384 rows came out
-// 9e-6 off, one over 1,024 rows 1e-6.  So a running sum is taken out of TMEM after kFlush * 64 rows and added in registers, rounded to
+// 9e-6 off, one over 1,024 rows 1e-6.  So a running sum is taken out of TMEM after 512 rows and added in registers, rounded to
 // nearest, while the next one grows in the other half of TMEM.
 //   Work is split by tile as long as there are tiles for all pairs; what is left (all of it, when weights are few and rows many) by
-// steps of 64 rows, partial tiles joined by a second kernel in a fixed order.
+// steps of 128 rows, partial tiles joined by a second kernel in a fixed order.
 #include <cuda.h>
 
 #include "ogq_act8.cuh"
@@ -19,9 +19,11 @@
 
 namespace ogq {
 
-constexpr int kStepRows = 64;                  // rows of t per stage
-constexpr int kFlush = 8;                      // stages per running sum
-constexpr int kOperands = 3;                   // converted tiles of x^: one being written by each warpgroup, one being multiplied
+// Rows of t per stage.  Each step costs the tensor cores about 110 ns besides its products (waits, commit, refilling their queue; 64 rows,
+// 320 ns of products: 16,384 x 4096 x 4096 480 us).
+constexpr int kStepRows = 128;
+constexpr int kFlush = 4;                      // steps per running sum
+constexpr int kOperands = 2;                   // converted tiles of x^: one being written, one being multiplied
 constexpr int kTileM = 256;                    // columns of dy per tile (both CTAs)
 constexpr int kABytes = 128 * kStepRows * 2;   // dy's tile of one CTA
 constexpr int kScaleBytes = kStepRows * 16;    // scales around those of a tile's (at most four) groups: 16 bytes a row by TMA, or two words
@@ -30,18 +32,16 @@ constexpr int kWgThreads = 640;                // a warpgroup for TMA, MMA, TMEM
 constexpr int kRegsStart = 96, kRegsControl = 48, kRegsConvert = 64, kRegsSums = 152;
 static_assert(128 * kRegsControl + 256 * kRegsConvert + 256 * kRegsSums <= kWgThreads * kRegsStart, "a warpgroup would wait for registers for ever");
 constexpr uint32_t kTmemColumns = 512;
-constexpr int kMinSteps = 8;                   // fewer steps than these are not split: a second launch costs more than they do
+constexpr int kMinSteps = 4;                   // fewer steps than these are not split: a second launch costs more than they do
 
 template <int BN> struct WgShape {
     static constexpr int kCols = BN / 2;                          // columns of x^ that one CTA converts
     static constexpr int kOcts = kCols / 8;                       // a converter thread has eight of them, in
     static constexpr int kRowsAtOnce = 128 / kOcts;               // rows row, row + kRowsAtOnce, ...
-    static constexpr int kRowsEach = kStepRows / kRowsAtOnce;
+    static constexpr int kRowsEach = kStepRows / 2 / kRowsAtOnce;  // of its warpgroup's half of the step
     static constexpr int kBBytes = kCols * kStepRows * 2;
     static constexpr int kRawBytes = kCols * kStepRows;
-    // Loads under way: a stage is in use from the request (2,200 cycles until the data is there when it comes from memory) until its
-    // product is done, some 3,600 cycles against 510 for the product itself; the converted tiles are needed for less than half of that.
-    static constexpr int kStages = BN == 256 ? 7 : 8;
+    static constexpr int kStages = BN == 256 ? 3 : 4;             // as many as fit: loads under way
     static constexpr int kSmem = kStages * (kABytes + kRawBytes + kScaleBytes) + kOperands * kBBytes + 1024;  // + alignment to the swizzle's 1024 bytes
     static_assert(kABytes % 1024 == 0 && kBBytes % 1024 == 0, "the swizzle goes by the address");
     static_assert(kSmem <= 226 * 1024, "shared memory");
@@ -57,7 +57,7 @@ struct WgArgs {
     int groups;         // of a row
     int tiles_m, tiles_n;
     int steps;          // of a tile: terms * steps_x
-    int steps_x;        // 64-row steps of x^
+    int steps_x;        // steps over x^'s rows
     int pairs;
     int whole;          // tiles per pair that are done alone
     int64_t rest;       // steps of the tiles left
@@ -209,9 +209,9 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
             mbar_init(dy_here(s), 1);
             mbar_init(done(s), 1);
             mbar_init(raw_here(s), a.tma_scales ? 1 : 33);  // TMA's, and those of the lanes that copy the scales
-            mbar_init(raw_free(s), 4);
+            mbar_init(raw_free(s), 8);
         }
-        for (int b = 0; b < kOperands; ++b) mbar_init(op_here(b), 8);
+        for (int b = 0; b < kOperands; ++b) mbar_init(op_here(b), 16);
         for (int d = 0; d < 2; ++d) {
             mbar_init(sum(d), 1);
             mbar_init(taken(d), 16);
@@ -315,7 +315,7 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
                 for (int k = w.k0; k < w.k1; ++k) {
                     if (!(ok = __all_sync(0xffffffffu, mbar_wait(raw_free(s), phase, &failed)))) break;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
+                    for (int r = 0; r < kStepRows / 16; ++r) {
                         const int row = lane + (r >> 1) * 32;
                         const int64_t t = (int64_t)x * kStepRows + row;
                         const int64_t at = ((t * a.groups + first) & ~(int64_t)3) + (r & 1) * 4;
@@ -328,24 +328,22 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
                 }
             }
         }
-    } else if (warp < 12) {  // converters: every other stage
+    } else if (warp < 12) {  // converters: each warpgroup half of the rows
         fewer_registers<kRegsConvert>();
-        const int which = (warp - 4) >> 2, id = threadIdx.x & 127;
-        const int oct = id % S::kOcts, row = id / S::kOcts;
+        const int id = threadIdx.x & 127;
+        const int oct = id % S::kOcts, row = ((warp - 4) >> 2) * (kStepRows / 2) + id / S::kOcts;
         WgWork w(a, pair);
         // the operand's place is free when the step kOperands before this one is done (none for the first kOperands)
-        int s = which, b = which, before = which + kStages - kOperands;
+        int s = 0, b = 0, before = kStages - kOperands;
         uint32_t phase = 0, before_phase = 1;
         bool ok = true;
-        int turn = which;  // steps until this warpgroup's next one
         while (ok && w.next(a, pair)) {
             int m, n;
             wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
             // this thread's byte of a row's; of words, the first holds the row's at a place that is the same eight rows on
             const int first = (n * BN + (int)rank * S::kCols) / kAct8Group;
             const int byte = (a.tma_scales ? first & 15 : (row * a.groups + first) & 3) + oct / 4;
-            int k = w.k0 + turn;
-            for (; k < w.k1; k += 2) {
+            for (int k = w.k0; k < w.k1; ++k) {
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(raw_here(s), phase, &failed) && mbar_wait(done(before), before_phase, &failed)))) break;
                 wg_convert<BN>(stage_raw(s), stage_scales(s) + byte, a.tma_scales ? 16 : 8, operand_b(b), row, oct);
                 fence_async_shared();
@@ -354,14 +352,10 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
                     mbar_arrive_cluster(map_to(op_here(b), 0));
                     mbar_arrive(raw_free(s));
                 }
-                s += 2;
-                if (s >= kStages) { s -= kStages; phase ^= 1; }
-                before += 2;
-                if (before >= kStages) { before -= kStages; before_phase ^= 1; }
-                b += 2;
-                if (b >= kOperands) b -= kOperands;
+                if (++s == kStages) { s = 0; phase ^= 1; }
+                if (++before == kStages) { before = 0; before_phase ^= 1; }
+                if (++b == kOperands) b = 0;
             }
-            turn = k - w.k1;
         }
     } else {  // sums out of TMEM, and out
         more_registers<kRegsSums>();
@@ -465,7 +459,7 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_join(const __grid_constant__
 
 // ---------------------------------------------------------------------------
 // Operands that TMA cannot read as they are (fp16, fp32, rows off 16-byte boundaries) are laid out in the scratch first:
-// dy as bf16 terms stacked along t, each of `padded` rows (a multiple of 64, zeros behind the last), and the codes with rows of
+// dy as bf16 terms stacked along t, each of `padded` rows (a multiple of a step's, zeros behind the last), and the codes with rows of
 // a multiple of 16 bytes; scales off 4-byte boundaries are copied too.
 // ---------------------------------------------------------------------------
 struct WgLayout {
@@ -630,7 +624,7 @@ Plan make_plan(int64_t rows, int64_t cols, int64_t out_cols, int dtype, bool lay
     if (lay_dy || lay_x || lay_s) {
         const int64_t per_row = (lay_dy ? p.terms * p.ld_terms * 2 : 0) + (lay_x ? p.ld_kept : 0) + (lay_s ? act8_groups(cols) : 0);
         int64_t most = kLayoutBytes / (per_row > 0 ? per_row : 1) / kStepRows * kStepRows;
-        if (most < 8 * kStepRows) most = 8 * kStepRows;
+        if (most < 4 * kStepRows) most = 4 * kStepRows;
         if (p.rows > most) p.rows = most;
     }
     const int64_t padded = up_to(p.rows, kStepRows);
