@@ -184,15 +184,29 @@ __device__ __forceinline__ void act8_values(uint2 c, float unit, float (&v)[8])
 
 // ---------------------------------------------------------------------------
 // Activation functions.  ACCURATE (fp32 activations): CUDA's own expf, erff and divisions.  Otherwise (results rounded to 8
-// or 11 bits): the fast exponential and division, and for Phi the rational form of Abramowitz and Stegun 7.1.26,
+// or 11 bits): the approximate exponential and reciprocal of the hardware, and for Phi the rational form of Abramowitz and Stegun 7.1.26,
 //   1 - Phi(|z|) = (a1 t + ... + a5 t^5) exp(-z^2/2) / 2,  t = 1 / (1 + p |z| / sqrt 2),  off by at most 7.5e-8,
 // which shares its exponential with the density in the slope.
 // ---------------------------------------------------------------------------
+__device__ __forceinline__ float fast_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_reciprocal(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.44269504f;
+
 template <bool ACCURATE>
 __device__ __forceinline__ float sigmoid(float z)
 {
     if constexpr (ACCURATE) return 1.f / (1.f + expf(-z));
-    return __fdividef(1.f, 1.f + __expf(-z));
+    return fast_reciprocal(__fadd_rn(1.f, fast_exp2(__fmul_rn(z, -kLog2e))));
 }
 
 // Phi(z), and exp(-z^2/2) in e
@@ -203,14 +217,14 @@ __device__ __forceinline__ float normal_cdf(float z, float& e)
         e = expf(-0.5f * z * z);
         return 0.5f * erfcf(-0.70710678118654752f * z);
     } else {
-        e = __expf(-0.5f * z * z);
-        const float t = __fdividef(1.f, __fmaf_rn(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
-        float p = __fmaf_rn(t, 1.061405429f, -1.453152027f);
-        p = __fmaf_rn(p, t, 1.421413741f);
-        p = __fmaf_rn(p, t, -0.284496736f);
-        p = __fmaf_rn(p, t, 0.254829592f);
-        const float tail = 0.5f * p * t * e;
-        return z < 0.f ? tail : 1.f - tail;
+        e = fast_exp2(__fmul_rn(__fmul_rn(z, -0.5f * kLog2e), z));
+        const float t = fast_reciprocal(__fmaf_rn(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
+        float p = __fmaf_rn(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+        p = __fmaf_rn(p, t, 0.5f * 1.421413741f);
+        p = __fmaf_rn(p, t, 0.5f * -0.284496736f);
+        p = __fmaf_rn(p, t, 0.5f * 0.254829592f);
+        const float tail = __fmul_rn(__fmul_rn(p, t), e);
+        return z < 0.f ? tail : __fsub_rn(1.f, tail);
     }
 }
 
@@ -221,7 +235,7 @@ __device__ __forceinline__ float act_value(float z)
     if constexpr (ACT == OGQ_ACT_RELU) return z > 0.f ? z : z == z ? 0.f : z;
     if constexpr (ACT == OGQ_ACT_SILU) {
         if constexpr (ACCURATE) return z / (1.f + expf(-z));
-        return __fdividef(z, 1.f + __expf(-z));
+        return __fmul_rn(z, sigmoid<false>(z));
     }
     if constexpr (ACT == OGQ_ACT_GELU) {
         float e;
@@ -263,6 +277,25 @@ __device__ __forceinline__ float act_both(float z, float& slope)
     }
     slope = act_slope<ACT, ACCURATE>(z);
     return act_value<ACT, ACCURATE>(z);
+}
+
+constexpr int kAct8Ctas = 16;  // per SM, at most, of the kernels that stream a matrix
+
+// g / d = hi(g * mul) >> shift for every g below 2^31 and d of 2 and more (d = 1 is not divided by).
+inline void act8_divisor(uint32_t d, uint32_t& mul, uint32_t& shift)
+{
+    mul = shift = 0;
+    if (d < 2) return;
+    shift = 0;
+    while ((2u << shift) < d) ++shift;  // 2^shift < d <= 2^(shift+1)
+    mul = (uint32_t)((((uint64_t)1 << (32 + shift)) + d - 1) / d);
+}
+
+// The row of group g.
+template <class A>
+__device__ __forceinline__ uint32_t act8_row(const A& a, uint32_t g)
+{
+    return a.groups == a.all_groups ? 0u : a.groups == 1 ? g : __umulhi(g, a.div_mul) >> a.div_shift;
 }
 
 // Calls f(std::integral_constant) for a run-time choice.

@@ -14,41 +14,119 @@ struct BwdArgs {
     int64_t ld_dy, ld_dx, ld_dup, cols;
     uint32_t groups;      // of a row
     uint32_t all_groups;  // of the matrix
+    uint32_t div_mul, div_shift;  // g / groups = hi(g * div_mul) >> div_shift
     int act;              // of the kernel of single elements
 };
 
-// Any sizes, strides and addresses: a warp per group, a lane per element.
+// Any sizes, strides and addresses: a warp per group, a lane per element, four groups under way.
 template <class E, bool GATED>
 __global__ void __launch_bounds__(kThreads) k_act8_backward_any(const __grid_constant__ BwdArgs a)
 {
     pdl_wait();
     pdl_launch_dependents();
     constexpr bool kAccurate = sizeof(E) == 4;
+    constexpr int kUnits = 4;
     const int lane = threadIdx.x & 31;
-    const uint32_t warps = gridDim.x * kWarps;
-    for (uint32_t g = blockIdx.x * kWarps + (threadIdx.x >> 5); g < a.all_groups; g += warps) {
-        const uint32_t row = g / a.groups;
-        const int64_t col = (int64_t)(g - row * a.groups) * kAct8Group + lane;
-        if (col >= a.cols) continue;
-        const int64_t at = (int64_t)row * a.cols + col;
-        const float x = (float)a.codes[at] * act8_unit(a.scales[g]);
-        float dx = x;
-        if (a.dy) {
-            const float dy = load1((const E*)a.dy + row * a.ld_dy + col);
-            float f = x, slope = 1.f;
-            switch (a.act) {
-                case OGQ_ACT_RELU: f = act_both<OGQ_ACT_RELU, kAccurate>(x, slope); break;
-                case OGQ_ACT_SILU: f = act_both<OGQ_ACT_SILU, kAccurate>(x, slope); break;
-                case OGQ_ACT_GELU: f = act_both<OGQ_ACT_GELU, kAccurate>(x, slope); break;
-            }
-            dx = dy;
-            if (GATED) {
-                dx *= (float)a.up_codes[at] * act8_unit(a.up_scales[g]);
-                store1((E*)a.dup + row * a.ld_dup + col, dy * f);
-            }
-            dx *= slope;
+    for (uint32_t g0 = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * kUnits; g0 < a.all_groups; g0 += gridDim.x * kWarps * kUnits) {
+        float v[kUnits], u[kUnits], d[kUnits];
+        uint32_t row[kUnits];
+        int64_t col[kUnits];
+        bool in[kUnits];
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            row[k] = act8_row(a, g0 + k);
+            col[k] = (int64_t)(g0 + k - row[k] * a.groups) * kAct8Group + lane;
+            in[k] = g0 + k < a.all_groups && col[k] < a.cols;
+            if (!in[k]) continue;
+            const int64_t at = (int64_t)row[k] * a.cols + col[k];
+            v[k] = (float)a.codes[at] * act8_unit(a.scales[g0 + k]);
+            if (GATED) u[k] = (float)a.up_codes[at] * act8_unit(a.up_scales[g0 + k]);
+            if (a.dy) d[k] = load1((const E*)a.dy + row[k] * a.ld_dy + col[k]);
         }
-        store1((E*)a.dx + row * a.ld_dx + col, dx);
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            if (!in[k]) continue;
+            float dx = v[k];
+            if (a.dy) {
+                float f = v[k], slope = 1.f;
+                switch (a.act) {
+                    case OGQ_ACT_RELU: f = act_both<OGQ_ACT_RELU, kAccurate>(f, slope); break;
+                    case OGQ_ACT_SILU: f = act_both<OGQ_ACT_SILU, kAccurate>(f, slope); break;
+                    case OGQ_ACT_GELU: f = act_both<OGQ_ACT_GELU, kAccurate>(f, slope); break;
+                }
+                dx = d[k];
+                if (GATED) {
+                    dx *= u[k];
+                    store1((E*)a.dup + row[k] * a.ld_dup + col[k], d[k] * f);
+                }
+                dx *= slope;
+            }
+            store1((E*)a.dx + row[k] * a.ld_dx + col[k], dx);
+        }
+    }
+}
+
+// Rows of whole eights of elements on 16-byte boundaries: eight elements a thread at a time, UNITS such pieces under way.
+template <class E, int ACT, bool GATED, bool DECODE>
+__global__ void __launch_bounds__(kThreads) k_act8_backward(const __grid_constant__ BwdArgs a)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr bool kAccurate = sizeof(E) == 4;
+    constexpr int kUnits = GATED || sizeof(E) == 4 ? 2 : 4;
+    const uint32_t team = threadIdx.x >> 2;
+    const int part = threadIdx.x & 3;
+    const uint32_t stride = kThreads / 4;
+    for (uint32_t g0 = blockIdx.x * (stride * kUnits) + team; g0 < a.all_groups; g0 += gridDim.x * (stride * kUnits)) {
+        Raw8<E> dy[DECODE ? 1 : kUnits];
+        uint2 x[kUnits], u[GATED ? kUnits : 1];
+        uint32_t sx[kUnits], su[GATED ? kUnits : 1];
+        int64_t row[kUnits], col[kUnits];
+        bool in[kUnits];
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            const uint32_t g = g0 + k * stride;
+            const uint32_t r = act8_row(a, g);
+            row[k] = r;
+            col[k] = (int64_t)(g - r * a.groups) * kAct8Group + part * 8;
+            in[k] = g < a.all_groups && col[k] < a.cols;
+            if (in[k]) {
+                const int64_t at = row[k] * a.cols + col[k];
+                x[k] = *reinterpret_cast<const uint2*>(a.codes + at);
+                sx[k] = a.scales[g];
+                if constexpr (GATED) {
+                    u[k] = *reinterpret_cast<const uint2*>(a.up_codes + at);
+                    su[k] = a.up_scales[g];
+                }
+                if constexpr (!DECODE) dy[k] = load_raw8((const E*)a.dy + row[k] * a.ld_dy + col[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            if (!in[k]) continue;
+            float v[8], d[8], w[8];
+            act8_values(x[k], act8_unit(sx[k]), v);
+            if constexpr (DECODE) {
+                store8((E*)a.dx + row[k] * a.ld_dx + col[k], v);
+            } else {
+                unpack8(dy[k], d);
+                if constexpr (GATED) {
+                    float dup[8];
+                    act8_values(u[k], act8_unit(su[k]), w);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        float slope;
+                        dup[j] = __fmul_rn(d[j], act_both<ACT, kAccurate>(v[j], slope));
+                        d[j] = __fmul_rn(__fmul_rn(d[j], w[j]), slope);
+                    }
+                    store8((E*)a.dup + row[k] * a.ld_dup + col[k], dup);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[j] = __fmul_rn(d[j], act_slope<ACT, kAccurate>(v[j]));
+                }
+                store8((E*)a.dx + row[k] * a.ld_dx + col[k], d);
+            }
+        }
     }
 }
 
@@ -61,15 +139,39 @@ cudaError_t launch_act8_backward(const Act8Backward& p, int sm_count, cudaStream
     a.groups = (uint32_t)act8_groups(p.cols);
     a.all_groups = (uint32_t)(p.rows * a.groups);
     a.act = p.act;
-    const int64_t want = ((int64_t)a.all_groups + kWarps - 1) / kWarps;
-    const int ctas = (int)(want < (int64_t)sm_count * 8 ? want : (int64_t)sm_count * 8);
+    const size_t size = p.dtype == OGQ_F32 ? 4 : 2;
+    const auto whole = [&](const void* q, int64_t ld) { return ((uintptr_t)q & 15) == 0 && ld * size % 16 == 0; };
+    const bool vec = p.cols % 8 == 0 && whole(p.dx, p.ld_dx) && ((uintptr_t)p.codes & 7) == 0 && (!p.dy || whole(p.dy, p.ld_dy)) &&
+                     (!p.dup || (whole(p.dup, p.ld_dup) && ((uintptr_t)p.up_codes & 7) == 0));
+    if (vec && p.cols % kAct8Group == 0 && p.ld_dx == p.cols && (!p.dy || p.ld_dy == p.cols) && (!p.dup || p.ld_dup == p.cols)) {
+        a.groups = a.all_groups;  // one long row
+        a.cols = p.rows * p.cols;
+    }
+    act8_divisor(a.groups, a.div_mul, a.div_shift);
     launch_begin(p.dy ? "k_act8_backward" : "k_act8_decode", stream);
-    const cudaError_t e = with_dtype(p.dtype, [&](auto elem) {
-        using E = decltype(elem);
-        return with_bool(p.dup != nullptr, [&](auto gated) {
-            return launch_pdl(k_act8_backward_any<E, decltype(gated)::value>, ctas, kThreads, 0, stream, a);
+    cudaError_t e;
+    if (vec) {
+        const int64_t per = kThreads / 4 * (p.dup || size == 4 ? 2 : 4);
+        const int64_t want = ((int64_t)a.all_groups + per - 1) / per;
+        const int ctas = (int)(want < (int64_t)sm_count * kAct8Ctas ? want : (int64_t)sm_count * kAct8Ctas);
+        e = with_dtype(p.dtype, [&](auto elem) {
+            using E = decltype(elem);
+            if (!p.dy) return launch_pdl(k_act8_backward<E, OGQ_ACT_NONE, false, true>, ctas, kThreads, 0, stream, a);
+            return with_bool(p.dup != nullptr, [&](auto gated) {
+                return with_act(p.act, [&](auto act) {
+                    return launch_pdl(k_act8_backward<E, decltype(act)::value, decltype(gated)::value, false>, ctas, kThreads, 0, stream, a);
+                });
+            });
         });
-    });
+    } else {
+        const int64_t want = ((int64_t)a.all_groups + kWarps * 4 - 1) / (kWarps * 4);
+        const int ctas = (int)(want < (int64_t)sm_count * 8 ? want : (int64_t)sm_count * 8);
+        e = with_dtype(p.dtype, [&](auto elem) {
+            return with_bool(p.dup != nullptr, [&](auto gated) {
+                return launch_pdl(k_act8_backward_any<decltype(elem), decltype(gated)::value>, ctas, kThreads, 0, stream, a);
+            });
+        });
+    }
     launch_end(stream);
     return e;
 }

@@ -16,55 +16,125 @@ struct FwdArgs {
     uint32_t groups;      // of a row
     uint32_t all_groups;  // of the matrix
     uint32_t stream_id;
+    uint32_t div_mul, div_shift;  // g / groups = hi(g * div_mul) >> div_shift
     int act;              // of the kernel of single elements
     bool random;
     PhiloxKeys keys;
 };
 
-// Any sizes, strides and addresses: a warp per group, a lane per element.
+// Any sizes, strides and addresses: a warp per group, a lane per element, four groups under way.
 template <class E, bool GATED>
 __global__ void __launch_bounds__(kThreads) k_act8_forward_any(const __grid_constant__ FwdArgs a)
 {
     pdl_wait();
     pdl_launch_dependents();
     constexpr bool kAccurate = sizeof(E) == 4;
+    constexpr int kUnits = 4;
     const int lane = threadIdx.x & 31;
-    const uint32_t warps = gridDim.x * kWarps;
-    for (uint32_t g = blockIdx.x * kWarps + (threadIdx.x >> 5); g < a.all_groups; g += warps) {
-        const uint32_t row = g / a.groups;
-        const int64_t col = (int64_t)(g - row * a.groups) * kAct8Group + lane;
-        const bool in = col < a.cols;
-        const int64_t at = (int64_t)row * a.cols + col;
-        float v = 0.f, u = 0.f;
-        if (in) {
-            v = load1((const E*)a.x + row * a.ld_x + col);
-            if (GATED) u = load1((const E*)a.up + row * a.ld_up + col);
+    for (uint32_t g0 = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * kUnits; g0 < a.all_groups; g0 += gridDim.x * kWarps * kUnits) {
+        float v[kUnits], u[kUnits];
+        uint32_t row[kUnits];
+        int64_t col[kUnits];
+        bool in[kUnits];
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            row[k] = act8_row(a, g0 + k);
+            col[k] = (int64_t)(g0 + k - row[k] * a.groups) * kAct8Group + lane;
+            in[k] = g0 + k < a.all_groups && col[k] < a.cols;
+            v[k] = in[k] ? load1((const E*)a.x + row[k] * a.ld_x + col[k]) : 0.f;
+            u[k] = GATED && in[k] ? load1((const E*)a.up + row[k] * a.ld_up + col[k]) : 0.f;
         }
 #pragma unroll
-        for (int k = 0; k < (GATED ? 2 : 1); ++k) {
-            const float w = k ? u : v;
-            const uint32_t byte = act8_byte(__reduce_max_sync(0xffffffffu, abs_bits(w)));
-            uint32_t code;
-            if (a.random) {
-                const uint64_t block = (uint64_t)at / 4;
-                const uint4 r = philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), (uint32_t)k, a.stream_id, a.keys);
-                const uint32_t i = (uint32_t)at & 3u;
-                code = act8_code_random(w, byte, i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w);
-            } else {
-                code = act8_code(w, byte);
+        for (int k = 0; k < kUnits; ++k) {
+            const int64_t at = (int64_t)row[k] * a.cols + col[k];
+#pragma unroll
+            for (int h = 0; h < (GATED ? 2 : 1); ++h) {
+                const float w = h ? u[k] : v[k];
+                const uint32_t byte = act8_byte(__reduce_max_sync(0xffffffffu, abs_bits(w)));
+                uint32_t code;
+                if (a.random) {
+                    const uint64_t block = (uint64_t)at / 4;
+                    const uint4 r = philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), (uint32_t)h, a.stream_id, a.keys);
+                    const uint32_t i = (uint32_t)at & 3u;
+                    code = act8_code_random(w, byte, i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w);
+                } else {
+                    code = act8_code(w, byte);
+                }
+                if (in[k]) (h ? a.up_codes : a.codes)[at] = (int8_t)(uint8_t)code;
+                if (lane == 0 && in[k]) (h ? a.up_scales : a.scales)[g0 + k] = (uint8_t)byte;
             }
-            if (in) (k ? a.up_codes : a.codes)[at] = (int8_t)(uint8_t)code;
-            if (lane == 0) (k ? a.up_scales : a.scales)[g] = (uint8_t)byte;
+            if (in[k] && a.y) {
+                float y = v[k];
+                switch (a.act) {
+                    case OGQ_ACT_RELU: y = act_value<OGQ_ACT_RELU, kAccurate>(y); break;
+                    case OGQ_ACT_SILU: y = act_value<OGQ_ACT_SILU, kAccurate>(y); break;
+                    case OGQ_ACT_GELU: y = act_value<OGQ_ACT_GELU, kAccurate>(y); break;
+                }
+                if (GATED) y *= u[k];
+                store1((E*)a.y + row[k] * a.ld_y + col[k], y);
+            }
         }
-        if (in && a.y) {
-            float y = v;
-            switch (a.act) {
-                case OGQ_ACT_RELU: y = act_value<OGQ_ACT_RELU, kAccurate>(v); break;
-                case OGQ_ACT_SILU: y = act_value<OGQ_ACT_SILU, kAccurate>(v); break;
-                case OGQ_ACT_GELU: y = act_value<OGQ_ACT_GELU, kAccurate>(v); break;
+    }
+}
+
+// Rows of whole eights of elements on 16-byte boundaries: four lanes hold a group, eight elements each, and a thread has UNITS
+// groups under way.
+//   Bound by memory.  UNITS = 4 keeps 16 KB a CTA requested at once (8 KB each of x and up with a gate).
+template <class E, int ACT, bool GATED, bool RANDOM, bool HAS_Y>
+__global__ void __launch_bounds__(kThreads) k_act8_forward(const __grid_constant__ FwdArgs a)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr bool kAccurate = sizeof(E) == 4;
+    constexpr int kUnits = GATED || sizeof(E) == 4 ? 2 : 4;
+    const uint32_t team = threadIdx.x >> 2;
+    const int part = threadIdx.x & 3;
+    const uint32_t stride = kThreads / 4;
+    for (uint32_t g0 = blockIdx.x * (stride * kUnits) + team; __any_sync(0xffffffffu, g0 < a.all_groups); g0 += gridDim.x * (stride * kUnits)) {
+        Raw8<E> x[kUnits], u[GATED ? kUnits : 1];
+        int64_t row[kUnits], col[kUnits];
+        bool in[kUnits];
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            const uint32_t g = g0 + k * stride;
+            const uint32_t r = act8_row(a, g);
+            row[k] = r;
+            col[k] = (int64_t)(g - r * a.groups) * kAct8Group + part * 8;
+            in[k] = g < a.all_groups && col[k] < a.cols;
+            x[k] = in[k] ? load_raw8((const E*)a.x + row[k] * a.ld_x + col[k]) : zero_raw8<E>();
+            if constexpr (GATED) u[k] = in[k] ? load_raw8((const E*)a.up + row[k] * a.ld_up + col[k]) : zero_raw8<E>();
+        }
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            const uint32_t g = g0 + k * stride;
+            const int64_t at = row[k] * a.cols + col[k];
+            float v[8], w[8];
+            unpack8(x[k], v);
+            if constexpr (GATED) unpack8(u[k], w);
+#pragma unroll
+            for (int h = 0; h < (GATED ? 2 : 1); ++h) {
+                const float(&z)[8] = h ? w : v;
+                uint32_t m = max_abs_bits(z);
+                m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                const uint32_t byte = act8_byte(m);
+                const uint2 c = act8_codes<RANDOM>(z, byte, (uint64_t)at, (uint32_t)h, a.stream_id, a.keys);
+                if (in[k]) {
+                    *reinterpret_cast<uint2*>((h ? a.up_codes : a.codes) + at) = c;
+                    if (part == 0) (h ? a.up_scales : a.scales)[g] = (uint8_t)byte;
+                }
             }
-            if (GATED) y *= u;
-            store1((E*)a.y + row * a.ld_y + col, y);
+            if constexpr (HAS_Y) {
+                if (in[k]) {
+                    float y[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        y[j] = act_value<ACT, kAccurate>(v[j]);
+                        if constexpr (GATED) y[j] = __fmul_rn(y[j], w[j]);
+                    }
+                    store8((E*)a.y + row[k] * a.ld_y + col[k], y);
+                }
+            }
         }
     }
 }
@@ -81,15 +151,42 @@ cudaError_t launch_act8_forward(const Act8Forward& p, int sm_count, cudaStream_t
     a.act = p.act;
     a.random = p.rounding == OGQ_ROUND_RANDOM;
     a.keys = philox_round_keys((uint32_t)p.seed, (uint32_t)(p.seed >> 32));
-    const int64_t want = ((int64_t)a.all_groups + kWarps - 1) / kWarps;
-    const int ctas = (int)(want < (int64_t)sm_count * 8 ? want : (int64_t)sm_count * 8);
+    const size_t size = p.dtype == OGQ_F32 ? 4 : 2;
+    const auto whole = [&](const void* q, int64_t ld) { return ((uintptr_t)q & 15) == 0 && ld * size % 16 == 0; };
+    const bool vec = p.cols % 8 == 0 && whole(p.x, p.ld_x) && ((uintptr_t)p.codes & 7) == 0 && (!p.y || whole(p.y, p.ld_y)) &&
+                     (!p.up || (whole(p.up, p.ld_up) && ((uintptr_t)p.up_codes & 7) == 0));
+    if (vec && p.cols % kAct8Group == 0 && p.ld_x == p.cols && (!p.y || p.ld_y == p.cols) && (!p.up || p.ld_up == p.cols)) {
+        a.groups = a.all_groups;  // one long row
+        a.cols = p.rows * p.cols;
+    }
+    act8_divisor(a.groups, a.div_mul, a.div_shift);
     launch_begin("k_act8_forward", stream);
-    const cudaError_t e = with_dtype(p.dtype, [&](auto elem) {
-        using E = decltype(elem);
-        return with_bool(p.up != nullptr, [&](auto gated) {
-            return launch_pdl(k_act8_forward_any<E, decltype(gated)::value>, ctas, kThreads, 0, stream, a);
+    cudaError_t e;
+    if (vec) {
+        const int64_t per = kThreads / 4 * (p.up || size == 4 ? 2 : 4);
+        const int64_t want = ((int64_t)a.all_groups + per - 1) / per;
+        const int ctas = (int)(want < (int64_t)sm_count * kAct8Ctas ? want : (int64_t)sm_count * kAct8Ctas);
+        e = with_dtype(p.dtype, [&](auto elem) {
+            using E = decltype(elem);
+            return with_bool(a.random, [&](auto random) {
+                constexpr bool R = decltype(random)::value;
+                if (!p.y) return launch_pdl(k_act8_forward<E, OGQ_ACT_NONE, false, R, false>, ctas, kThreads, 0, stream, a);
+                return with_bool(p.up != nullptr, [&](auto gated) {
+                    return with_act(p.act, [&](auto act) {
+                        return launch_pdl(k_act8_forward<E, decltype(act)::value, decltype(gated)::value, R, true>, ctas, kThreads, 0, stream, a);
+                    });
+                });
+            });
         });
-    });
+    } else {
+        const int64_t want = ((int64_t)a.all_groups + kWarps * 4 - 1) / (kWarps * 4);
+        const int ctas = (int)(want < (int64_t)sm_count * 8 ? want : (int64_t)sm_count * 8);
+        e = with_dtype(p.dtype, [&](auto elem) {
+            return with_bool(p.up != nullptr, [&](auto gated) {
+                return launch_pdl(k_act8_forward_any<decltype(elem), decltype(gated)::value>, ctas, kThreads, 0, stream, a);
+            });
+        });
+    }
     launch_end(stream);
     return e;
 }
