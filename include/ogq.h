@@ -360,7 +360,7 @@ ogq_status ogq_act8_wgrad(const void *d_dy, int64_t ld_dy, const int8_t *d_codes
  *             dx = rstd (gamma_c dz - m1 - xh m2),  m1, m2 = the means of gamma dz and gamma dz xh over the group.
  *             d_dgamma and d_dbeta fp32 [C], overwritten; each may be NULL.
  * The variance is taken about the mean (no difference of large sums).  N, P or C may be 0 (sums over nothing are 0, so is the mean).
- * G divides C, eps > 0.  P C/G is below 2^31 and N * ceil(C/32) * P below 2^31 (OGQ_ERR_UNSUPPORTED).  The order of the additions
+ * G divides C, eps > 0.  P C/G, N G and N * ceil(C/32) * P are below 2^31 (OGQ_ERR_UNSUPPORTED).  The order of the additions
  * depends on the sizes and the number of SMs only.  d_ws: scratch of ogq_group_norm_workspace_bytes, 256-byte aligned.
  * d_y may be d_x and d_dx may be d_dy; outputs overlap nothing else.
  */

@@ -183,10 +183,13 @@ __device__ __forceinline__ void act8_values(uint2 c, float unit, float (&v)[8])
 }
 
 // ---------------------------------------------------------------------------
-// Activation functions.  ACCURATE (fp32 activations): CUDA's own expf, erff and divisions.  Otherwise (results rounded to 8
-// or 11 bits): the approximate exponential and reciprocal of the hardware, and for Phi the rational form of Abramowitz and Stegun 7.1.26,
-//   1 - Phi(|z|) = (a1 t + ... + a5 t^5) exp(-z^2/2) / 2,  t = 1 / (1 + p |z| / sqrt 2),  off by at most 7.5e-8,
-// which shares its exponential with the density in the slope.
+// Activation functions, with the hardware's approximate exponential and reciprocal (2^-22 and 2^-23; the argument's rounding adds
+// |z| 2^-24).  Phi, the normal distribution function, from 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2:
+//   ACCURATE (fp32 activations): the Chebyshev fit of Numerical Recipes' erfcc, erfc(x) = t exp(-x^2 + p(t)), t = 1 / (1 + x / 2), p of
+//   degree 9, off by at most 1.2e-7 of the value, far tails included.  (CUDA's erfcf and expf: 54 us for the forward pass of
+//   group norm with GELU on 16.8 M fp32 values that is bound by memory at 30.)
+//   Otherwise (results rounded to 8 or 11 bits): Abramowitz and Stegun 7.1.26, erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2),
+//   t = 1 / (1 + p x), off by at most 1.5e-7, which shares its exponential with the density in the slope.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float fast_exp2(float x)
 {
@@ -202,10 +205,8 @@ __device__ __forceinline__ float fast_reciprocal(float x)
 }
 constexpr float kLog2e = 1.44269504f;
 
-template <bool ACCURATE>
 __device__ __forceinline__ float sigmoid(float z)
 {
-    if constexpr (ACCURATE) return 1.f / (1.f + expf(-z));
     return fast_reciprocal(__fadd_rn(1.f, fast_exp2(__fmul_rn(z, -kLog2e))));
 }
 
@@ -213,19 +214,30 @@ __device__ __forceinline__ float sigmoid(float z)
 template <bool ACCURATE>
 __device__ __forceinline__ float normal_cdf(float z, float& e)
 {
+    e = fast_exp2(__fmul_rn(__fmul_rn(z, -0.5f * kLog2e), z));
+    float tail;
     if constexpr (ACCURATE) {
-        e = expf(-0.5f * z * z);
-        return 0.5f * erfcf(-0.70710678118654752f * z);
+        const float x = fabsf(z) * 0.70710678118654752f;
+        const float t = fast_reciprocal(__fmaf_rn(x, 0.5f, 1.f));
+        float p = __fmaf_rn(t, 0.17087277f, -0.82215223f);
+        p = __fmaf_rn(p, t, 1.48851587f);
+        p = __fmaf_rn(p, t, -1.13520398f);
+        p = __fmaf_rn(p, t, 0.27886807f);
+        p = __fmaf_rn(p, t, -0.18628806f);
+        p = __fmaf_rn(p, t, 0.09678418f);
+        p = __fmaf_rn(p, t, 0.37409196f);
+        p = __fmaf_rn(p, t, 1.00002368f);
+        p = __fmaf_rn(p, t, -1.26551223f);
+        tail = __fmul_rn(0.5f * t, fast_exp2(__fmul_rn(__fmaf_rn(-x, x, p), kLog2e)));
     } else {
-        e = fast_exp2(__fmul_rn(__fmul_rn(z, -0.5f * kLog2e), z));
         const float t = fast_reciprocal(__fmaf_rn(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
         float p = __fmaf_rn(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
         p = __fmaf_rn(p, t, 0.5f * 1.421413741f);
         p = __fmaf_rn(p, t, 0.5f * -0.284496736f);
         p = __fmaf_rn(p, t, 0.5f * 0.254829592f);
-        const float tail = __fmul_rn(__fmul_rn(p, t), e);
-        return z < 0.f ? tail : __fsub_rn(1.f, tail);
+        tail = __fmul_rn(__fmul_rn(p, t), e);
     }
+    return z < 0.f ? tail : __fsub_rn(1.f, tail);
 }
 
 // f(z), and its slope in s
@@ -233,10 +245,7 @@ template <int ACT, bool ACCURATE>
 __device__ __forceinline__ float act_value(float z)
 {
     if constexpr (ACT == OGQ_ACT_RELU) return z > 0.f ? z : z == z ? 0.f : z;
-    if constexpr (ACT == OGQ_ACT_SILU) {
-        if constexpr (ACCURATE) return z / (1.f + expf(-z));
-        return __fmul_rn(z, sigmoid<false>(z));
-    }
+    if constexpr (ACT == OGQ_ACT_SILU) return __fmul_rn(z, sigmoid(z));
     if constexpr (ACT == OGQ_ACT_GELU) {
         float e;
         return z * normal_cdf<ACCURATE>(z, e);
@@ -249,7 +258,7 @@ __device__ __forceinline__ float act_slope(float z)
 {
     if constexpr (ACT == OGQ_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
     if constexpr (ACT == OGQ_ACT_SILU) {
-        const float s = sigmoid<ACCURATE>(z);
+        const float s = sigmoid(z);
         return s * __fmaf_rn(z, 1.f - s, 1.f);
     }
     if constexpr (ACT == OGQ_ACT_GELU) {
@@ -265,7 +274,7 @@ template <int ACT, bool ACCURATE>
 __device__ __forceinline__ float act_both(float z, float& slope)
 {
     if constexpr (ACT == OGQ_ACT_SILU) {
-        const float s = sigmoid<ACCURATE>(z);
+        const float s = sigmoid(z);
         slope = s * __fmaf_rn(z, 1.f - s, 1.f);
         return z * s;
     }

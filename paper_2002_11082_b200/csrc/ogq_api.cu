@@ -591,7 +591,7 @@ static ogq_status group_norm_sizes(int64_t N, int64_t P, int64_t C, int64_t G)
 {
     if (N < 0 || P < 0 || C < 0 || G < 1 || C % G != 0) return OGQ_ERR_INVALID_ARG;
     if (N >= kMaxGroups || P >= kMaxGroups || C >= kMaxGroups) return OGQ_ERR_UNSUPPORTED;
-    if (P * (C / G) >= kMaxGroups) return OGQ_ERR_UNSUPPORTED;
+    if (P * (C / G) >= kMaxGroups || N * G >= kMaxGroups) return OGQ_ERR_UNSUPPORTED;
     const int64_t per_pixel = (C + 31) / 32;
     if (P > 0 && N > 0 && per_pixel > 0 && (P >= kMaxGroups / N + 1 || N * P >= kMaxGroups || per_pixel >= kMaxGroups / (N * P) + 1 ||
                                             N * P * per_pixel >= kMaxGroups))

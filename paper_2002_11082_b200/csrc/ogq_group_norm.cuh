@@ -18,6 +18,7 @@ struct GnTiles {
 };
 
 constexpr int kGnMinPx = 16, kGnMaxPx = 64;  // pixels a thread: sums in fp32 stay short, partial sums stay few
+constexpr int kGnBatch = 4;                  // of them are loaded at once
 
 inline GnTiles gn_tiles(int64_t N, int64_t P, int64_t C, int64_t G, int V, int sm_count)
 {
@@ -121,26 +122,11 @@ __device__ __forceinline__ GnPlace gn_place(const GnTiles& t)
 }
 
 template <class E, int V>
-__device__ __forceinline__ void gn_load(const E* p, float (&v)[V])
-{
-    if constexpr (V == 8) unpack8(load_raw8(p), v);
-    else v[0] = load1(p);
-}
-template <class E, int V>
 __device__ __forceinline__ void gn_store(E* p, const float (&v)[V])
 {
     if constexpr (V == 8) store8(p, v);
     else store1(p, v[0]);
 }
-// The kept values of pixel `row` (of all samples') at channel c
-template <int V>
-__device__ __forceinline__ void gn_kept(const int8_t* codes, const uint8_t* scales, int64_t row, int64_t C, int64_t c, float (&v)[V])
-{
-    const float unit = act8_unit(scales[row * act8_groups(C) + c / kAct8Group]);
-    if constexpr (V == 8) act8_values(*reinterpret_cast<const uint2*>(codes + row * C + c), unit, v);
-    else v[0] = (float)codes[row * C + c] * unit;
-}
-
 // ACT < 0: chosen by `act` at run time (the kernels of single channels)
 template <int ACT, bool ACCURATE>
 __device__ __forceinline__ float gn_value(int act, float z)
@@ -165,15 +151,17 @@ __device__ __forceinline__ float gn_slope(int act, float z)
     }
 }
 
-// Parameters and statistics of V channels from c on, of sample n.
-template <int V>
+// Parameters and statistics of V channels from c on, of sample n, and xh = (x - mean) rstd.  fp32 activations: the difference
+// first, which is exact where x is near the mean.  16-bit ones: one multiply-add with mean rstd, off by 2^-24 |mean| rstd where
+// their own rounding is 2^-9 or 2^-12 |x| rstd.
+template <int V, bool ACCURATE>
 struct GnChannels {
-    float mean[V], rstd[V], gamma[V], beta[V];
+    float mean[V], rstd[V], gamma[V], beta[V];  // not ACCURATE: mean holds -mean rstd
     __device__ __forceinline__ void load(const GnArgs& a, int64_t n, int64_t c)
     {
-        const int64_t per = a.t.C / a.t.G;
-        int64_t g = c / per;
-        int64_t left = (g + 1) * per - c;  // channels until the next group
+        const int per = (int)(a.t.C / a.t.G);
+        int g = (int)c / per;
+        int left = (g + 1) * per - (int)c;  // channels until the next group
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             if (left == 0) { ++g; left = per; }
@@ -182,8 +170,66 @@ struct GnChannels {
             rstd[j] = a.rstd[n * a.t.G + g];
             gamma[j] = a.gamma ? a.gamma[c + j] : 1.f;
             beta[j] = a.beta ? a.beta[c + j] : 0.f;
+            if constexpr (!ACCURATE) mean[j] = __fmul_rn(-mean[j], rstd[j]);
         }
     }
+    __device__ __forceinline__ float xh(float x, int j) const
+    {
+        if constexpr (ACCURATE) return __fmul_rn(__fsub_rn(x, mean[j]), rstd[j]);
+        return __fmaf_rn(x, rstd[j], mean[j]);
+    }
 };
+
+// z = xh gamma + beta of V channels, for the forward pass: one multiply-add more than the difference, or none.
+template <int V, bool ACCURATE>
+struct GnAffine {
+    float mean[V], scale[V], shift[V];
+    __device__ __forceinline__ void set(int j, float m, float rstd, float gamma, float beta)
+    {
+        mean[j] = m;
+        scale[j] = __fmul_rn(rstd, gamma);
+        shift[j] = ACCURATE ? beta : __fmaf_rn(-m, scale[j], beta);
+    }
+    __device__ __forceinline__ float z(float x, int j) const
+    {
+        return __fmaf_rn(ACCURATE ? __fsub_rn(x, mean[j]) : x, scale[j], shift[j]);
+    }
+};
+
+// V elements as they lie in memory.
+template <class E, int V> struct GnRaw { E e; };
+template <class E> struct GnRaw<E, 8> { Raw8<E> e; };
+template <class E, int V>
+__device__ __forceinline__ GnRaw<E, V> gn_fetch(const E* p)
+{
+    GnRaw<E, V> r;
+    if constexpr (V == 8) r.e = load_raw8(p);
+    else r.e = *p;
+    return r;
+}
+template <class E, int V>
+__device__ __forceinline__ void gn_open(const GnRaw<E, V>& r, float (&v)[V])
+{
+    if constexpr (V == 8) unpack8(r.e, v);
+    else v[0] = load1(&r.e);
+}
+// The same of kept values.
+template <int V> struct GnKept { int8_t c; uint32_t s; };
+template <> struct GnKept<8> { uint2 c; uint32_t s; };
+template <int V>
+__device__ __forceinline__ GnKept<V> gn_fetch_kept(const int8_t* codes, const uint8_t* scales, int64_t row, int64_t C, int64_t groups, int64_t c)
+{
+    GnKept<V> r;
+    if constexpr (V == 8) r.c = *reinterpret_cast<const uint2*>(codes + row * C + c);
+    else r.c = codes[row * C + c];
+    r.s = scales[row * groups + c / kAct8Group];
+    return r;
+}
+template <int V>
+__device__ __forceinline__ void gn_open(const GnKept<V>& r, float (&v)[V])
+{
+    if constexpr (V == 8) act8_values(r.c, act8_unit(r.s), v);
+    else v[0] = (float)r.c * act8_unit(r.s);
+}
 
 }  // namespace ogq

@@ -3,45 +3,66 @@
 //   dx = rstd (gamma dz - m1 - xh m2),  m1, m2 = means over the group of gamma dz and gamma dz xh,
 // which are sums over the group's channels of gamma times the channel's two sums.
 // Any shape in three steps: both sums per channel of a chunk of pixels; joined per group and over the samples; the elements.
-#include "ogq_group_norm.cuh"
+#include <stdlib.h>
+#include "ogq_group_norm_resident.cuh"
 
 namespace ogq {
 
-// dz and xh of V channels of a pixel
-template <class E, int V, int ACT, bool KEPT>
-__device__ __forceinline__ void gn_dz(const GnArgs& a, int64_t row, int64_t c, const GnChannels<V>& ch, float (&dz)[V], float (&xh)[V])
-{
-    constexpr bool kAccurate = sizeof(E) == 4;
-    gn_load((const E*)a.dy + row * a.t.C + c, dz);
-    if constexpr (KEPT) gn_kept(a.codes, a.scales, row, a.t.C, c, xh);
-    else gn_load((const E*)a.x + row * a.t.C + c, xh);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        xh[j] = __fmul_rn(__fsub_rn(xh[j], ch.mean[j]), ch.rstd[j]);
-        dz[j] = __fmul_rn(dz[j], gn_slope<ACT, kAccurate>(a.act, __fmaf_rn(xh[j], ch.gamma[j], ch.beta[j])));
+// What the backward pass reads of V channels of a pixel: dy, and x as it is or as it was kept.
+template <class E, int V, bool KEPT>
+struct GnPair {
+    GnRaw<E, V> dy;
+    std::conditional_t<KEPT, GnKept<V>, GnRaw<E, V>> x;
+    __device__ __forceinline__ void fetch(const GnArgs& a, int64_t row, int64_t c, int64_t groups)
+    {
+        dy = gn_fetch<E, V>((const E*)a.dy + row * a.t.C + c);
+        if constexpr (KEPT) x = gn_fetch_kept<V>(a.codes, a.scales, row, a.t.C, groups, c);
+        else x = gn_fetch<E, V>((const E*)a.x + row * a.t.C + c);
     }
-}
+    template <int ACT, bool ACCURATE>
+    __device__ __forceinline__ void open(int act, const GnChannels<V, ACCURATE>& ch, float (&dz)[V], float (&xh)[V]) const
+    {
+        gn_open<E, V>(dy, dz);
+        if constexpr (KEPT) gn_open<V>(x, xh);
+        else gn_open<E, V>(x, xh);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            xh[j] = ch.xh(xh[j], j);
+            dz[j] = __fmul_rn(dz[j], gn_slope<ACT, ACCURATE>(act, __fmaf_rn(xh[j], ch.gamma[j], ch.beta[j])));
+        }
+    }
+};
 
 template <class E, int V, int ACT, bool KEPT>
 __global__ void __launch_bounds__(kThreads) k_gn_grad_sums(const __grid_constant__ GnArgs a)
 {
     pdl_wait();
     pdl_launch_dependents();
+    constexpr bool kAccurate = sizeof(E) == 4;
     __shared__ float2 sh[kThreads * V];
     const GnPlace q = gn_place<V>(a.t);
+    const int64_t groups = act8_groups(a.t.C);
     if (q.active) {
-        GnChannels<V> ch;
+        GnChannels<V, kAccurate> ch;
         ch.load(a, q.n, q.c);
         float sb[V], sg[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) sb[j] = sg[j] = 0.f;
-        for (int64_t p = q.first; p < q.last; p += a.t.ty) {
-            float dz[V], xh[V];
-            gn_dz<E, V, ACT, KEPT>(a, q.n * a.t.P + p, q.c, ch, dz, xh);
+        for (int64_t p = q.first; p < q.last; p += kGnBatch * a.t.ty) {
+            GnPair<E, V, KEPT> r[kGnBatch];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                sb[j] = __fadd_rn(sb[j], dz[j]);
-                sg[j] = __fmaf_rn(dz[j], xh[j], sg[j]);
+            for (int k = 0; k < kGnBatch; ++k)
+                if (p + k * a.t.ty < q.last) r[k].fetch(a, q.n * a.t.P + p + k * a.t.ty, q.c, groups);
+#pragma unroll
+            for (int k = 0; k < kGnBatch; ++k) {
+                if (p + k * a.t.ty >= q.last) break;
+                float dz[V], xh[V];
+                r[k].template open<ACT, kAccurate>(a.act, ch, dz, xh);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    sb[j] = __fadd_rn(sb[j], dz[j]);
+                    sg[j] = __fmaf_rn(dz[j], xh[j], sg[j]);
+                }
             }
         }
 #pragma unroll
@@ -62,50 +83,67 @@ __global__ void __launch_bounds__(kThreads) k_gn_grad_sums(const __grid_constant
     }
 }
 
-// The first CTAs: a warp per sample and group, m1 and m2.  The others: dgamma and dbeta of 32 channels each.
+// The first CTAs: one per sample and group, m1 and m2.  The others: dgamma and dbeta of eight channels each, 32 rows of partial
+// sums at a time.
 __global__ void __launch_bounds__(kThreads) k_gn_grad_join(const __grid_constant__ GnArgs a, int group_ctas)
 {
     pdl_wait();
     pdl_launch_dependents();
+    __shared__ double sh[2][kThreads];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if ((int)blockIdx.x < group_ctas) {
-        const int64_t w = (int64_t)blockIdx.x * kWarps + warp;
-        if (w >= a.N * a.t.G) return;
-        const int64_t n = w / a.t.G, g = w - n * a.t.G, per = a.t.C / a.t.G;
-        const int64_t entries = a.t.chunks * per;
-        const float2* part = a.part + n * a.t.chunks * a.t.C + g * per;
+        const int64_t w = blockIdx.x;
+        const int n = (int)(w / a.t.G), g = (int)(w - n * a.t.G), per = (int)(a.t.C / a.t.G);
+        const int64_t entries = (int64_t)a.t.chunks * per;
+        const float2* part = a.part + (int64_t)n * a.t.chunks * a.t.C + (int64_t)g * per;
         double s1 = 0.0, s2 = 0.0;
-        for (int64_t i = lane; i < entries; i += 32) {
-            const int64_t k = i / per, c = i - k * per;
-            const float2 e = __ldcg(part + k * a.t.C + c);
-            const double gamma = a.gamma ? (double)a.gamma[g * per + c] : 1.0;
+#pragma unroll 4
+        for (int64_t i = threadIdx.x; i < entries; i += kThreads) {
+            const uint32_t k = (uint32_t)i / (uint32_t)per, c = (uint32_t)i - k * per;
+            const float2 e = __ldcg(part + (int64_t)k * a.t.C + c);
+            const double gamma = a.gamma ? (double)a.gamma[(int64_t)g * per + c] : 1.0;
             s1 += gamma * (double)e.x;
             s2 += gamma * (double)e.y;
         }
         s1 = warp_sum(s1);
         s2 = warp_sum(s2);
+        if (lane == 0) {
+            sh[0][warp] = s1;
+            sh[1][warp] = s2;
+        }
+        __syncthreads();
         const double m = (double)(a.t.P * per);
-        if (lane == 0) a.sums[w] = make_float2((float)(s1 / m), (float)(s2 / m));
+        if (threadIdx.x == 0) {
+            s1 = s2 = 0.0;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) {
+                s1 += sh[0][i];
+                s2 += sh[1][i];
+            }
+            a.sums[w] = make_float2((float)(s1 / m), (float)(s2 / m));
+        }
         return;
     }
-    __shared__ double sh[2][kWarps][32];
-    const int64_t c = (int64_t)((int)blockIdx.x - group_ctas) * 32 + lane;
+    const int64_t c = (int64_t)((int)blockIdx.x - group_ctas) * 8 + (threadIdx.x & 7);
     double sb = 0.0, sg = 0.0;
     if (c < a.t.C) {
-        for (int64_t r = warp; r < a.N * a.t.chunks; r += kWarps) {
+#pragma unroll 4
+        for (int64_t r = threadIdx.x >> 3; r < a.N * a.t.chunks; r += kThreads / 8) {
             const float2 e = __ldcg(a.part + r * a.t.C + c);
             sb += (double)e.x;
             sg += (double)e.y;
         }
     }
-    sh[0][warp][lane] = sb;
-    sh[1][warp][lane] = sg;
+    sh[0][threadIdx.x] = sb;
+    sh[1][threadIdx.x] = sg;
     __syncthreads();
-    if (warp < 2 && c < a.t.C) {
+    if (threadIdx.x < 16) {  // eight channels of both
+        const int which = threadIdx.x >> 3;
+        const int64_t o = (int64_t)((int)blockIdx.x - group_ctas) * 8 + (threadIdx.x & 7);
         double s = 0.0;
-        for (int k = 0; k < kWarps; ++k) s += sh[warp][k][lane];
-        float* out = warp ? a.dgamma : a.dbeta;
-        if (out) out[c] = (float)s;
+        for (int k = 0; k < kThreads / 8; ++k) s += sh[which][k * 8 + (threadIdx.x & 7)];
+        float* out = which ? a.dgamma : a.dbeta;
+        if (out && o < a.t.C) out[o] = (float)s;
     }
 }
 
@@ -114,26 +152,170 @@ __global__ void __launch_bounds__(kThreads) k_gn_grad(const __grid_constant__ Gn
 {
     pdl_wait();
     pdl_launch_dependents();
+    constexpr bool kAccurate = sizeof(E) == 4;
     const GnPlace q = gn_place<V>(a.t);
     if (!q.active) return;
-    GnChannels<V> ch;
+    const int64_t groups = act8_groups(a.t.C);
+    GnChannels<V, kAccurate> ch;
     ch.load(a, q.n, q.c);
-    float m1[V], m2[V];
-    const int64_t per = a.t.C / a.t.G;
+    float c0[V], c1[V], c2[V];  // dx = dz c1 - xh c2 - c0
+    const int per = (int)(a.t.C / a.t.G);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const float2 s = __ldcg(a.sums + q.n * a.t.G + (q.c + j) / per);
-        m1[j] = s.x;
-        m2[j] = s.y;
+        const float2 s = __ldcg(a.sums + q.n * a.t.G + ((int)q.c + j) / per);
+        c0[j] = __fmul_rn(-s.x, ch.rstd[j]);
+        c1[j] = __fmul_rn(ch.gamma[j], ch.rstd[j]);
+        c2[j] = __fmul_rn(-s.y, ch.rstd[j]);
     }
-    for (int64_t p = q.first; p < q.last; p += a.t.ty) {
-        const int64_t row = q.n * a.t.P + p;
-        float dz[V], xh[V], dx[V];
-        gn_dz<E, V, ACT, KEPT>(a, row, q.c, ch, dz, xh);
+    for (int64_t p = q.first; p < q.last; p += kGnBatch * a.t.ty) {
+        GnPair<E, V, KEPT> r[kGnBatch];
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            dx[j] = __fmul_rn(ch.rstd[j], __fmaf_rn(-xh[j], m2[j], __fmaf_rn(dz[j], ch.gamma[j], -m1[j])));
-        gn_store((E*)a.out + row * a.t.C + q.c, dx);
+        for (int k = 0; k < kGnBatch; ++k)
+            if (p + k * a.t.ty < q.last) r[k].fetch(a, q.n * a.t.P + p + k * a.t.ty, q.c, groups);
+#pragma unroll
+        for (int k = 0; k < kGnBatch; ++k) {
+            if (p + k * a.t.ty >= q.last) break;
+            float dz[V], xh[V];
+            r[k].template open<ACT, kAccurate>(a.act, ch, dz, xh);
+#pragma unroll
+            for (int j = 0; j < V; ++j) dz[j] = __fmaf_rn(dz[j], c1[j], __fmaf_rn(xh[j], c2[j], c0[j]));
+            gn_store((E*)a.out + (q.n * a.t.P + p + k * a.t.ty) * a.t.C + q.c, dz);
+        }
+    }
+}
+
+// The whole pass of one slab (see ogq_group_norm_resident.cuh): dy and x are read once, dz stays in fp32 registers (its slope costs
+// more than its 8 registers a vector), xh is computed again from x.
+template <class E, int ACT, bool KEPT, int U>
+__global__ void __launch_bounds__(kThreads, 2) k_gn_backward(const __grid_constant__ GnArgs a, const __grid_constant__ GnSlab s)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr bool kAccurate = sizeof(E) == 4;
+    __shared__ float2 sh[kThreads * 8];
+    __shared__ float2 sh_cta[kGnMaxWidth], sh_all[kGnMaxWidth], sh_group[kGnMaxWidth];
+    const GnSpot q = gn_spot(a.t, s);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int groups = s.width / s.per;
+    Raw8<E> rdy[U], rx[KEPT ? 1 : U];
+    uint2 kx[KEPT ? U : 1];
+    uint32_t ks[KEPT ? U : 1];
+    bool in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t p = q.first + q.ty + u * s.rows;
+        in[u] = q.active && p < q.last;
+        const int64_t row = q.n * a.t.P + p;
+        rdy[u] = in[u] ? load_raw8((const E*)a.dy + row * a.t.C + q.c) : zero_raw8<E>();
+        if constexpr (KEPT) {
+            kx[u] = make_uint2(0u, 0u);
+            ks[u] = 0u;
+            if (in[u]) {
+                kx[u] = *reinterpret_cast<const uint2*>(a.codes + row * a.t.C + q.c);
+                ks[u] = a.scales[row * act8_groups(a.t.C) + q.c / kAct8Group];
+            }
+        } else {
+            rx[u] = in[u] ? load_raw8((const E*)a.x + row * a.t.C + q.c) : zero_raw8<E>();
+        }
+    }
+    GnChannels<8, kAccurate> ch;
+    if (q.active) ch.load(a, q.n, q.c);
+    float dz[U][8];
+    float2 sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[8];
+        unpack8(rdy[u], dz[u]);
+        if constexpr (KEPT) act8_values(kx[u], act8_unit(ks[u]), f);
+        else unpack8(rx[u], f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float xh = ch.xh(f[j], j);
+            dz[u][j] = __fmul_rn(dz[u][j], act_slope<ACT, kAccurate>(__fmaf_rn(xh, ch.gamma[j], ch.beta[j])));
+            if (in[u]) {
+                sum[j].x = __fadd_rn(sum[j].x, dz[u][j]);
+                sum[j].y = __fmaf_rn(dz[u][j], xh, sum[j].y);
+            }
+        }
+    }
+    gn_put_sums(s, q, sum, sh, s.width);
+    __syncthreads();
+    for (int c = threadIdx.x; c < s.width; c += kThreads) {
+        float2 t = make_float2(0.f, 0.f);
+        for (int r = 0; r < s.sum_rows; ++r) {
+            const float2 e = sh[r * s.width + c];
+            t.x += e.x;
+            t.y += e.y;
+        }
+        sh_cta[c] = t;
+    }
+    if (s.cluster > 1) {
+        gn_cluster_arrive();
+        gn_cluster_wait();
+    } else {
+        __syncthreads();
+    }
+    for (int c = threadIdx.x; c < s.width; c += kThreads) {
+        float2 t = sh_cta[c];
+        if (s.cluster > 1) {
+            t = make_float2(0.f, 0.f);
+            for (int r = 0; r < s.cluster; ++r) {
+                const float2 e = gn_remote(&sh_cta[c], r);
+                t.x += e.x;
+                t.y += e.y;
+            }
+        }
+        const int64_t at = q.c - q.c0 + c;
+        if (q.rank == 0) a.part[q.n * a.t.C + at] = t;
+        const float gamma = a.gamma ? a.gamma[at] : 1.f;
+        sh_all[c] = make_float2(gamma * t.x, gamma * t.y);
+    }
+    __syncthreads();
+    if (s.cluster > 1) gn_cluster_arrive();  // this CTA has read the others' sums
+    for (int g = warp; g < groups; g += kWarps) {
+        float2 t = make_float2(0.f, 0.f);
+        for (int c = lane; c < s.per; c += 32) {
+            t.x += sh_all[g * s.per + c].x;
+            t.y += sh_all[g * s.per + c].y;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
+            t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
+        }
+        const float m = (float)(a.t.P * s.per);
+        if (lane == 0) sh_group[g] = make_float2(t.x / m, t.y / m);
+    }
+    __syncthreads();
+    if (q.active) {
+        float2 g[8];
+        int k = q.c0 / s.per, left = (k + 1) * s.per - q.c0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (left == 0) { ++k; left = s.per; }
+            --left;
+            g[j] = sh_group[k];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!in[u]) continue;
+            const int64_t row = q.n * a.t.P + q.first + q.ty + u * s.rows;
+            float f[8];
+            if constexpr (KEPT) act8_values(kx[u], act8_unit(ks[u]), f);
+            else unpack8(rx[u], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float xh = ch.xh(f[j], j);
+                f[j] = __fmul_rn(ch.rstd[j], __fmaf_rn(-xh, g[j].y, __fmaf_rn(dz[u][j], ch.gamma[j], -g[j].x)));
+            }
+            store8((E*)a.out + row * a.t.C + q.c, f);
+        }
+    }
+    if (s.cluster > 1) {
+        __syncwarp();
+        gn_cluster_wait();  // the others have read this CTA's
     }
 }
 
@@ -143,7 +325,37 @@ cudaError_t launch_group_norm_backward(const GroupNorm& p, int sm_count, cudaStr
     const bool kept = p.codes != nullptr;
     const bool vec = p.C % 8 == 0 && gn_aligned(p.dy, 16) && gn_aligned(p.out, 16) && (p.C * size) % 16 == 0 &&
                      (kept ? gn_aligned(p.codes, 8) : gn_aligned(p.x, 16));
-    const GnArgs a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, vec ? 8 : 1, sm_count));
+    GnArgs a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, vec ? 8 : 1, sm_count));
+    const int channel_ctas = p.dgamma || p.dbeta ? (int)((p.C + 7) / 8) : 0;
+    GnSlab slab;
+    if (vec && a.t.ctas > 0) {
+        const int most = size == 4 ? 4 : 8;  // vectors a thread can hold
+        int u = 0;
+        if (gn_slab(p.N, p.P, p.C, p.G, (int)size, false, 2, slab) && slab.ctas <= (int64_t)sm_count * kGnFewCtas) u = 2;
+        else if (getenv("GN_MOST") && gn_slab(p.N, p.P, p.C, p.G, (int)size, false, most, slab)) u = most;
+        if (u) {
+            launch_begin("k_gn_backward", stream);
+            cudaError_t e = with_dtype(p.dtype, [&](auto elem) {
+                using E = decltype(elem);
+                constexpr int M = sizeof(E) == 4 ? 4 : 8;
+                return with_act(p.act, [&](auto act) {
+                    constexpr int A = decltype(act)::value;
+                    return with_bool(kept, [&](auto k) {
+                        constexpr bool K = decltype(k)::value;
+                        return u == 2 ? launch_cluster(k_gn_backward<E, A, K, 2>, slab.ctas, slab.cluster, stream, a, slab)
+                                      : launch_cluster(k_gn_backward<E, A, K, M>, slab.ctas, slab.cluster, stream, a, slab);
+                    });
+                });
+            });
+            launch_end(stream);
+            if (e != cudaSuccess || channel_ctas == 0) return e;
+            a.t.chunks = 1;  // a pair of sums per sample and channel
+            launch_begin("k_gn_grad_join", stream);
+            e = launch_pdl(k_gn_grad_join, channel_ctas, kThreads, 0, stream, a, 0);
+            launch_end(stream);
+            return e;
+        }
+    }
     const auto launch = [&](auto which) {
         constexpr bool kSums = decltype(which)::value;
         return with_dtype(p.dtype, [&](auto elem) {
@@ -165,8 +377,7 @@ cudaError_t launch_group_norm_backward(const GroupNorm& p, int sm_count, cudaStr
         launch_end(stream);
         if (e != cudaSuccess) return e;
     }
-    const int group_ctas = a.t.ctas > 0 ? (int)((p.N * p.G + kWarps - 1) / kWarps) : 0;
-    const int channel_ctas = p.dgamma || p.dbeta ? (int)((p.C + 31) / 32) : 0;
+    const int group_ctas = a.t.ctas > 0 ? (int)(p.N * p.G) : 0;
     if (group_ctas + channel_ctas > 0) {
         launch_begin("k_gn_grad_join", stream);
         e = launch_pdl(k_gn_grad_join, group_ctas + channel_ctas, kThreads, 0, stream, a, group_ctas);

@@ -4,7 +4,8 @@
 //   Moments are sums about the first value a thread sees: that value is one of those summed, so the sum of squares about the
 // mean is at least (1 - 1/n) of its squared distance d to the mean, while what is subtracted is n d^2: with n <= 64 pixels a thread the
 // difference loses at most a factor 64 of fp32's 2^-24.  Joining two sets adds n_a n_b / (n_a + n_b) (mean_a - mean_b)^2, all positive.
-#include "ogq_group_norm.cuh"
+#include <stdlib.h>
+#include "ogq_group_norm_resident.cuh"
 
 namespace ogq {
 
@@ -21,15 +22,27 @@ __global__ void __launch_bounds__(kThreads) k_gn_moments(const __grid_constant__
         const E* x = (const E*)a.x + q.n * a.t.P * a.t.C + q.c;
 #pragma unroll
         for (int j = 0; j < V; ++j) s1[j] = s2[j] = shift[j] = 0.f;
-        for (int64_t p = q.first; p < q.last; p += a.t.ty, ++n) {
-            float v[V];
-            gn_load(x + p * a.t.C, v);
+        for (int64_t p = q.first; p < q.last; p += kGnBatch * a.t.ty) {
+            GnRaw<E, V> r[kGnBatch];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if (n == 0) shift[j] = v[j];
-                const float d = __fsub_rn(v[j], shift[j]);
-                s1[j] = __fadd_rn(s1[j], d);
-                s2[j] = __fmaf_rn(d, d, s2[j]);
+            for (int k = 0; k < kGnBatch; ++k)
+                if (p + k * a.t.ty < q.last) r[k] = gn_fetch<E, V>(x + (p + k * a.t.ty) * a.t.C);
+#pragma unroll
+            for (int k = 0; k < kGnBatch; ++k) {
+                if (p + k * a.t.ty >= q.last) break;
+                float v[V];
+                gn_open<E, V>(r[k], v);
+                if (k == 0 && n == 0) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) shift[j] = v[j];
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float d = __fsub_rn(v[j], shift[j]);
+                    s1[j] = __fadd_rn(s1[j], d);
+                    s2[j] = __fmaf_rn(d, d, s2[j]);
+                }
+                ++n;
             }
         }
 #pragma unroll
@@ -59,36 +72,65 @@ __global__ void __launch_bounds__(kThreads) k_gn_moments(const __grid_constant__
     }
 }
 
-// A warp per sample and group: joins the channels and chunks.
+// A CTA per sample and group: joins the channels and chunks.
 __global__ void __launch_bounds__(kThreads) k_gn_stats(const __grid_constant__ GnArgs a)
 {
     pdl_wait();
     pdl_launch_dependents();
-    const int lane = threadIdx.x & 31;
-    const int64_t w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    if (w >= a.N * a.t.G) return;
-    const int64_t n = w / a.t.G, g = w - n * a.t.G, per = a.t.C / a.t.G;
+    __shared__ double scratch[2][kWarps];
+    const int64_t w = blockIdx.x;
+    const int n = (int)(w / a.t.G), g = (int)(w - n * a.t.G), per = (int)(a.t.C / a.t.G);
     const int64_t px = (int64_t)a.t.ty * a.t.px;
-    const int64_t entries = a.t.chunks * per;
-    const float2* part = a.part + n * a.t.chunks * a.t.C + g * per;
+    const int64_t entries = (int64_t)a.t.chunks * per;  // below 2^31: no more than P C / G
+    const float2* part = a.part + (int64_t)n * a.t.chunks * a.t.C + (int64_t)g * per;
+    const auto entry = [&](int64_t i, double& count) {
+        const uint32_t k = (uint32_t)i / (uint32_t)per, c = (uint32_t)i - k * per;
+        count = (double)((k + 1) * px < a.t.P ? px : a.t.P - k * px);
+        return __ldcg(part + (int64_t)k * a.t.C + c);
+    };
+    constexpr int kKeep = 4;  // entries a thread keeps between the two sums
+    float2 kept[kKeep];
+    double counts[kKeep];
     double sum = 0.0;
-    for (int64_t i = lane; i < entries; i += 32) {
-        const int64_t k = i / per, c = i - k * per;
-        const int64_t count = (k + 1) * px < a.t.P ? px : a.t.P - k * px;
-        sum += (double)count * (double)__ldcg(part + k * a.t.C + c).x;
+#pragma unroll
+    for (int u = 0; u < kKeep; ++u) {
+        counts[u] = 0.0;
+        kept[u] = make_float2(0.f, 0.f);
+        if (threadIdx.x + u * kThreads < entries) kept[u] = entry(threadIdx.x + u * kThreads, counts[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kKeep; ++u)
+        if (counts[u] > 0.0) sum += counts[u] * (double)kept[u].x;
+    for (int64_t i = threadIdx.x + kKeep * kThreads; i < entries; i += kThreads) {
+        double count;
+        const float2 e = entry(i, count);
+        sum += count * (double)e.x;
     }
     const double m = (double)(a.t.P * per);
-    const double mean = m > 0 ? warp_sum(sum) / m : 0.0;
+    const auto total = [&](double v, double* sh) {
+        v = warp_sum(v);
+        if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+        __syncthreads();
+        double t = 0.0;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) t += sh[i];
+        return t;
+    };
+    const double mean = m > 0 ? total(sum, scratch[0]) / m : 0.0;
     double m2 = 0.0;
-    for (int64_t i = lane; i < entries; i += 32) {
-        const int64_t k = i / per, c = i - k * per;
-        const int64_t count = (k + 1) * px < a.t.P ? px : a.t.P - k * px;
-        const float2 e = __ldcg(part + k * a.t.C + c);
-        const double d = (double)e.x - mean;
-        m2 += (double)e.y + (double)count * d * d;
+#pragma unroll
+    for (int u = 0; u < kKeep; ++u) {
+        const double d = (double)kept[u].x - mean;
+        if (counts[u] > 0.0) m2 += (double)kept[u].y + counts[u] * d * d;
     }
-    m2 = warp_sum(m2);
-    if (lane == 0) {
+    for (int64_t i = threadIdx.x + kKeep * kThreads; i < entries; i += kThreads) {
+        double count;
+        const float2 e = entry(i, count);
+        const double d = (double)e.x - mean;
+        m2 += (double)e.y + count * d * d;
+    }
+    m2 = total(m2, scratch[1]);
+    if (threadIdx.x == 0) {
         a.mean[w] = (float)mean;
         a.rstd[w] = (float)(1.0 / sqrt((m > 0 ? m2 / m : 0.0) + (double)a.eps));
     }
@@ -103,25 +145,191 @@ __global__ void __launch_bounds__(kThreads) k_gn_apply(const __grid_constant__ G
     constexpr bool kAccurate = sizeof(E) == 4;
     const GnPlace q = gn_place<V>(a.t);
     if (!q.active) return;  // KEEP: whole groups of lanes, since tx is a multiple of 4
-    GnChannels<V> ch;
-    ch.load(a, q.n, q.c);
-    float scale[V];
+    GnAffine<V, kAccurate> f;
+    {
+        const int per = (int)(a.t.C / a.t.G);
+        int g = (int)q.c / per, left = (g + 1) * per - (int)q.c;
 #pragma unroll
-    for (int j = 0; j < V; ++j) scale[j] = ch.rstd[j] * ch.gamma[j];
-    const unsigned team = 0xfu << (threadIdx.x & 28);
-    for (int64_t p = q.first; p < q.last; p += a.t.ty) {
-        const int64_t row = q.n * a.t.P + p;
-        float v[V], y[V];
-        gn_load((const E*)a.x + row * a.t.C + q.c, v);
-#pragma unroll
-        for (int j = 0; j < V; ++j) y[j] = gn_value<ACT, kAccurate>(a.act, __fmaf_rn(__fsub_rn(v[j], ch.mean[j]), scale[j], ch.beta[j]));
-        if constexpr (KEEP != 0 && V == 8) {
-            const uint32_t byte = act8_byte(__reduce_max_sync(team, max_abs_bits(v)));
-            *reinterpret_cast<uint2*>(a.codes + row * a.t.C + q.c) =
-                act8_codes<KEEP == 2>(v, byte, (uint64_t)(row * a.t.C + q.c), 0u, a.stream_id, a.keys);
-            if ((threadIdx.x & 3) == 0) a.scales[(row * a.t.C + q.c) / kAct8Group] = (uint8_t)byte;
+        for (int j = 0; j < V; ++j) {
+            if (left == 0) { ++g; left = per; }
+            --left;
+            const int64_t at = q.n * a.t.G + g;
+            f.set(j, __ldcg(a.mean + at), __ldcg(a.rstd + at), a.gamma ? a.gamma[q.c + j] : 1.f, a.beta ? a.beta[q.c + j] : 0.f);
         }
-        gn_store((E*)a.out + row * a.t.C + q.c, y);
+    }
+    const unsigned team = 0xfu << (threadIdx.x & 28);
+    for (int64_t p = q.first; p < q.last; p += kGnBatch * a.t.ty) {
+        const int64_t at = (q.n * a.t.P + p) * a.t.C + q.c, step = a.t.ty * a.t.C;
+        GnRaw<E, V> r[kGnBatch];
+#pragma unroll
+        for (int k = 0; k < kGnBatch; ++k)
+            if (p + k * a.t.ty < q.last) r[k] = gn_fetch<E, V>((const E*)a.x + at + k * step);
+#pragma unroll
+        for (int k = 0; k < kGnBatch; ++k) {
+            if (p + k * a.t.ty >= q.last) break;
+            float v[V], y[V];
+            gn_open<E, V>(r[k], v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) y[j] = gn_value<ACT, kAccurate>(a.act, f.z(v[j], j));
+            if constexpr (KEEP != 0 && V == 8) {
+                uint32_t b = max_abs_bits(v);
+                b = max(b, __shfl_xor_sync(team, b, 1));
+                b = max(b, __shfl_xor_sync(team, b, 2));
+                const uint32_t byte = act8_byte(b);
+                *reinterpret_cast<uint2*>(a.codes + at + k * step) = act8_codes<KEEP == 2>(v, byte, (uint64_t)(at + k * step), 0u, a.stream_id, a.keys);
+                if ((threadIdx.x & 3) == 0) a.scales[(at + k * step) / kAct8Group] = (uint8_t)byte;
+            }
+            gn_store((E*)a.out + at + k * step, y);
+        }
+    }
+}
+
+// The whole pass of one slab (see ogq_group_norm_resident.cuh): x is read once.  The CTA's mean and its sum of squares about that
+// mean, then joined over the cluster.
+template <class E, int ACT, int KEEP, int U>
+__global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : 3) k_gn_forward(const __grid_constant__ GnArgs a, const __grid_constant__ GnSlab s)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr bool kAccurate = sizeof(E) == 4;
+    __shared__ float sh[kThreads * 8];
+    __shared__ float sh_mean[kGnMaxWidth], sh_rstd[kGnMaxWidth];
+    __shared__ float2 sh_cta[kGnMaxWidth];
+    const GnSpot q = gn_spot(a.t, s);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int groups = s.width / s.per;
+    const E* x = (const E*)a.x + q.n * a.t.P * a.t.C + q.c;
+    Raw8<E> v[U];
+    bool in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t p = q.first + q.ty + u * s.rows;
+        in[u] = q.active && p < q.last;
+        v[u] = in[u] ? load_raw8(x + p * a.t.C) : zero_raw8<E>();
+    }
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[8];
+        unpack8(v[u], f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = __fadd_rn(sum[j], f[j]);  // pixels that are not there count 0
+    }
+    gn_put_sums(s, q, sum, sh, s.width);
+    __syncthreads();
+    const float count = (float)((int)(q.last - q.first) * s.per);
+    for (int g = warp; g < groups; g += kWarps) {
+        float t = 0.f;
+        for (int c = lane; c < s.per; c += 32)
+            for (int r = 0; r < s.sum_rows; ++r) t += sh[r * s.width + g * s.per + c];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+        if (lane == 0) sh_mean[g] = count > 0.f ? t / count : 0.f;
+    }
+    __syncthreads();
+    float m[8];
+    {
+        int g = q.c0 / s.per, left = (g + 1) * s.per - q.c0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (left == 0) { ++g; left = s.per; }
+            --left;
+            m[j] = sh_mean[g];
+            sum[j] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[8];
+        unpack8(v[u], f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float d = in[u] ? __fsub_rn(f[j], m[j]) : 0.f;
+            sum[j] = __fmaf_rn(d, d, sum[j]);
+        }
+    }
+    gn_put_sums(s, q, sum, sh, s.width);
+    __syncthreads();
+    for (int g = warp; g < groups; g += kWarps) {
+        float t = 0.f;
+        for (int c = lane; c < s.per; c += 32)
+            for (int r = 0; r < s.sum_rows; ++r) t += sh[r * s.width + g * s.per + c];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+        if (lane == 0) sh_cta[g] = make_float2(sh_mean[g], t);
+    }
+    if (s.cluster > 1) {
+        gn_cluster_arrive();
+        gn_cluster_wait();
+    } else {
+        __syncthreads();
+    }
+    for (int g = warp; g < groups; g += kWarps) {  // a lane per CTA of the cluster
+        float2 e = make_float2(0.f, 0.f);
+        float n = 0.f;
+        if (lane < s.cluster) {
+            e = s.cluster > 1 ? gn_remote(&sh_cta[g], lane) : sh_cta[g];
+            const int64_t first = (int64_t)lane * s.share, last = first + s.share < a.t.P ? first + s.share : a.t.P;
+            n = last > first ? (float)((int)(last - first) * s.per) : 0.f;
+        }
+        const float all = (float)(a.t.P * s.per);
+        float mean = n > 0.f ? n * e.x : 0.f;
+#pragma unroll
+        for (int o = kGnMaxCluster / 2; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
+        mean = __shfl_sync(0xffffffffu, mean, 0) / all;
+        const float d = e.x - mean;
+        float m2 = n > 0.f ? __fmaf_rn(n * d, d, e.y) : 0.f;
+#pragma unroll
+        for (int o = kGnMaxCluster / 2; o > 0; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+        if (lane == 0) {
+            const float rstd = 1.f / sqrtf(m2 / all + a.eps);
+            sh_mean[g] = mean;
+            sh_rstd[g] = rstd;
+            if (q.rank == 0) {
+                const int64_t at = q.n * a.t.G + (q.c - q.c0) / s.per + g;
+                a.mean[at] = mean;
+                a.rstd[at] = rstd;
+            }
+        }
+    }
+    __syncthreads();
+    if (s.cluster > 1) gn_cluster_arrive();  // this CTA has read the others' sums
+    if (q.active) {
+        GnAffine<8, kAccurate> z;
+        int g = q.c0 / s.per, left = (g + 1) * s.per - q.c0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (left == 0) { ++g; left = s.per; }
+            --left;
+            z.set(j, sh_mean[g], sh_rstd[g], a.gamma ? a.gamma[q.c + j] : 1.f, a.beta ? a.beta[q.c + j] : 0.f);
+        }
+        const unsigned team = 0xfu << (threadIdx.x & 28);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t row = q.n * a.t.P + q.first + q.ty + u * s.rows;
+            float f[8], y[8];
+            unpack8(v[u], f);
+            if constexpr (KEEP != 0) {  // four lanes hold a group of 32 channels; the same pixel, so all four are in or none is
+                uint32_t b = max_abs_bits(f);
+                b = max(b, __shfl_xor_sync(team, b, 1));
+                b = max(b, __shfl_xor_sync(team, b, 2));
+                const uint32_t byte = act8_byte(b);
+                if (in[u]) {
+                    *reinterpret_cast<uint2*>(a.codes + row * a.t.C + q.c) =
+                        act8_codes<KEEP == 2>(f, byte, (uint64_t)(row * a.t.C + q.c), 0u, a.stream_id, a.keys);
+                    if ((threadIdx.x & 3) == 0) a.scales[(row * a.t.C + q.c) / kAct8Group] = (uint8_t)byte;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = act_value<ACT, kAccurate>(z.z(f[j], j));
+            if (in[u]) store8((E*)a.out + row * a.t.C + q.c, y);
+        }
+    }
+    if (s.cluster > 1) {
+        __syncwarp();
+        gn_cluster_wait();  // the others have read this CTA's
     }
 }
 
@@ -136,6 +344,33 @@ cudaError_t launch_group_norm_forward(const GroupNorm& p, int sm_count, cudaStre
     const size_t size = p.dtype == OGQ_F32 ? 4 : 2;
     const bool vec = p.C % 8 == 0 && gn_aligned(p.x, 16) && gn_aligned(p.out, 16) && (p.C * size) % 16 == 0;
     const bool fused = p.codes && vec && p.C % kAct8Group == 0 && gn_aligned(p.codes, 8);
+    GnSlab slab;
+    const int most = size == 4 ? 4 : 8;  // vectors a thread can hold
+    if (vec && p.P > 0 && (!p.codes || fused)) {
+        // few CTAs: two vectors a thread, which makes more of them and each quicker
+        int u = 0;
+        if (gn_slab(p.N, p.P, p.C, p.G, (int)size, fused, 2, slab) && slab.ctas <= (int64_t)sm_count * kGnFewCtas) u = 2;
+        else if (getenv("GN_MOST") && gn_slab(p.N, p.P, p.C, p.G, (int)size, fused, most, slab)) u = most;
+        if (u) {
+            const GnArgs a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, 8, sm_count));
+            launch_begin("k_gn_forward", stream);
+            const cudaError_t e = with_dtype(p.dtype, [&](auto elem) {
+                using E = decltype(elem);
+                constexpr int M = sizeof(E) == 4 ? 4 : 8;
+                return with_act(p.act, [&](auto act) {
+                    constexpr int A = decltype(act)::value;
+                    return with_bool(u == 2, [&](auto few) {
+                        constexpr int U = decltype(few)::value ? 2 : M;
+                        if (!fused) return launch_cluster(k_gn_forward<E, A, 0, U>, slab.ctas, slab.cluster, stream, a, slab);
+                        if (p.rounding == OGQ_ROUND_RANDOM) return launch_cluster(k_gn_forward<E, A, 2, U>, slab.ctas, slab.cluster, stream, a, slab);
+                        return launch_cluster(k_gn_forward<E, A, 1, U>, slab.ctas, slab.cluster, stream, a, slab);
+                    });
+                });
+            });
+            launch_end(stream);
+            return e;
+        }
+    }
     cudaError_t e = cudaSuccess;
     if (p.codes && !fused && p.P > 0) {  // before the elements: y may be x
         Act8Forward f = {};
@@ -157,7 +392,7 @@ cudaError_t launch_group_norm_forward(const GroupNorm& p, int sm_count, cudaStre
         if (e != cudaSuccess) return e;
     }
     launch_begin("k_gn_stats", stream);
-    e = launch_pdl(k_gn_stats, (int)((p.N * p.G + kWarps - 1) / kWarps), kThreads, 0, stream, a);
+    e = launch_pdl(k_gn_stats, (int)(p.N * p.G), kThreads, 0, stream, a);
     launch_end(stream);
     if (e != cudaSuccess || a.t.ctas == 0) return e;
     launch_begin("k_gn_apply", stream);
