@@ -151,9 +151,7 @@ __device__ __forceinline__ uint2 act8_codes(const float (&v)[8], uint32_t byte, 
             c[4 * h + 2] = act8_code_random(v[4 * h + 2], byte, r.z);
             c[4 * h + 3] = act8_code_random(v[4 * h + 3], byte, r.w);
         }
-    } else if (byte == kAct8NanByte) {
-        return make_uint2(0u, 0u);
-    } else if (byte == kAct8MaxByte) {
+    } else if (byte >= kAct8MaxByte) {  // seldom
 #pragma unroll
         for (int i = 0; i < 8; ++i) c[i] = act8_code(v[i], byte);
     } else {
@@ -171,6 +169,24 @@ __device__ __forceinline__ uint32_t max_abs_bits(const float (&v)[8])
 #pragma unroll
     for (int i = 1; i < 8; ++i) m = max(m, abs_bits(v[i]));
     return m;
+}
+
+// The same of eight values as they lie in memory: magnitudes of 16-bit types compare as whole numbers, two at a time.
+__device__ __forceinline__ uint32_t max_abs_bits(const Raw8<float>& r)
+{
+    const uint32_t k = 0x7fffffffu;
+    return max(max(max(r.a.x & k, r.a.y & k), max(r.a.z & k, r.a.w & k)), max(max(r.b.x & k, r.b.y & k), max(r.b.z & k, r.b.w & k)));
+}
+__device__ __forceinline__ uint32_t max_abs_16(const uint4& a)
+{
+    const uint32_t k = 0x7fff7fffu;
+    const uint32_t m = __vmaxu2(__vmaxu2(a.x & k, a.y & k), __vmaxu2(a.z & k, a.w & k));
+    return max(m & 0xffffu, m >> 16);
+}
+__device__ __forceinline__ uint32_t max_abs_bits(const Raw8<__nv_bfloat16>& r) { return max_abs_16(r.a) << 16; }
+__device__ __forceinline__ uint32_t max_abs_bits(const Raw8<__half>& r)
+{
+    return __float_as_uint(__half2float(__ushort_as_half((unsigned short)max_abs_16(r.a))));
 }
 
 // Values of eight codes: byte u = code + 128 as the low mantissa bits of 2^23, less 2^23 + 128, is exact.
@@ -258,8 +274,8 @@ __device__ __forceinline__ float act_slope(float z)
 {
     if constexpr (ACT == OGQ_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
     if constexpr (ACT == OGQ_ACT_SILU) {
-        const float s = sigmoid(z);
-        return s * __fmaf_rn(z, 1.f - s, 1.f);
+        const float s = sigmoid(z), t = __fmul_rn(z, s);
+        return __fmaf_rn(-t, s, __fadd_rn(s, t));
     }
     if constexpr (ACT == OGQ_ACT_GELU) {
         float e;
@@ -274,9 +290,9 @@ template <int ACT, bool ACCURATE>
 __device__ __forceinline__ float act_both(float z, float& slope)
 {
     if constexpr (ACT == OGQ_ACT_SILU) {
-        const float s = sigmoid(z);
-        slope = s * __fmaf_rn(z, 1.f - s, 1.f);
-        return z * s;
+        const float s = sigmoid(z), t = __fmul_rn(z, s);
+        slope = __fmaf_rn(-t, s, __fadd_rn(s, t));
+        return t;
     }
     if constexpr (ACT == OGQ_ACT_GELU) {
         float e;

@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(kThreads) k_act8_forward(const __grid_constant
 #pragma unroll
             for (int h = 0; h < (GATED ? 2 : 1); ++h) {
                 const float(&z)[8] = h ? w : v;
-                uint32_t m = max_abs_bits(z);
+                uint32_t m = max_abs_bits(h ? u[GATED ? k : 0] : x[k]);
                 m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
                 m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
                 const uint32_t byte = act8_byte(m);

@@ -17,10 +17,12 @@ struct GnTiles {
     int64_t ctas;
 };
 
-constexpr int kGnMinPx = 16, kGnMaxPx = 64;  // pixels a thread: sums in fp32 stay short, partial sums stay few
-constexpr int kGnBatch = 4;                  // of them are loaded at once
+constexpr int kGnMinPx = 16, kGnMaxPx = 64;  // pixels a thread where sums are taken: those in fp32 stay short, partial sums stay few
+constexpr int kGnMinPxApply = 4;             // where not
 
-inline GnTiles gn_tiles(int64_t N, int64_t P, int64_t C, int64_t G, int V, int sm_count)
+// Tiles for a kernel of which `wave` CTAs run at a time: whole waves, as near as the sizes allow (25.7 M bf16 values, moments: 800
+// CTAs on 592 places took 19 us, 576 take 12), of at least `least` pixels a thread.
+inline GnTiles gn_tiles(int64_t N, int64_t P, int64_t C, int64_t G, int V, int64_t wave, int least)
 {
     GnTiles t;
     t.P = P; t.C = C; t.G = G;
@@ -28,13 +30,29 @@ inline GnTiles gn_tiles(int64_t N, int64_t P, int64_t C, int64_t G, int V, int s
     t.tx = t.cv < kThreads ? t.cv : kThreads;
     t.ty = kThreads / t.tx;
     t.ctiles = (t.cv + t.tx - 1) / t.tx;
-    t.px = kGnMaxPx;
-    for (;; t.px /= 2) {
-        t.chunks = (int)((P + (int64_t)t.ty * t.px - 1) / ((int64_t)t.ty * t.px));
-        t.ctas = N * t.chunks * t.ctiles;
-        if (t.ctas >= (int64_t)sm_count * 4 || t.px == kGnMinPx) break;
+    const int64_t units = (P + t.ty - 1) / t.ty, tasks = N * t.ctiles;  // pixels a thread of a sample, samples and tiles across
+    int64_t px = kGnMaxPx;
+    if (tasks > 0) {
+        for (int64_t waves = 1; waves <= 16; ++waves) {
+            const int64_t chunks = wave * waves / tasks;
+            if (chunks == 0) continue;
+            const int64_t q = (units + chunks - 1) / chunks;
+            if (q <= kGnMaxPx) { px = q; break; }
+        }
     }
+    t.px = (int)(px < least ? least : px);
+    t.chunks = (int)((units + t.px - 1) / t.px);
+    t.ctas = tasks * t.chunks;
     return t;
+}
+
+// CTAs of a kernel that run at a time (looked up once per kernel).
+template <class K>
+inline int64_t gn_wave(K kernel, int sm_count)
+{
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kThreads, 0) != cudaSuccess || n < 1) n = 1;
+    return (int64_t)n * sm_count;
 }
 
 // Scratch: a pair per sample, chunk of pixels and channel, and a pair per sample and group.
@@ -94,31 +112,60 @@ inline GnArgs gn_args(const GroupNorm& p, const GnTiles& t)
 
 inline bool gn_aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
-// This thread's place: sample, pixels first, first + ty, ... below last, first channel c (active: it has any).
+// This thread's place: sample, chunk, and its pixels: the first one's row of the matrix [N P, C], how many (each ty rows on), channel c.
 struct GnPlace {
-    int64_t n;
-    int chunk, tx, ty;
-    int64_t first, last, c;
+    int64_t row;
+    int64_t c;
+    int n, chunk, tile, tx, ty, count;
     bool active;
 };
 template <int V>
 __device__ __forceinline__ GnPlace gn_place(const GnTiles& t)
 {
     GnPlace q;
-    const int64_t b = blockIdx.x;
-    const int64_t nc = b / t.ctiles;
-    const int tile = (int)(b - nc * t.ctiles);
-    q.n = nc / t.chunks;
-    q.chunk = (int)(nc - q.n * t.chunks);
-    q.ty = threadIdx.x / t.tx;
-    q.tx = threadIdx.x - q.ty * t.tx;
-    const int64_t begin = (int64_t)q.chunk * t.ty * t.px;
-    q.first = begin + q.ty;
-    q.last = begin + (int64_t)t.ty * t.px < t.P ? begin + (int64_t)t.ty * t.px : t.P;
-    const int cv = tile * t.tx + q.tx;
+    uint32_t nc = blockIdx.x;
+    q.tile = 0;
+    if (t.ctiles > 1) {
+        nc = blockIdx.x / (uint32_t)t.ctiles;
+        q.tile = (int)(blockIdx.x - nc * (uint32_t)t.ctiles);
+    }
+    q.n = (int)(nc / (uint32_t)t.chunks);
+    q.chunk = (int)(nc - (uint32_t)q.n * (uint32_t)t.chunks);
+    q.ty = (int)(threadIdx.x / (uint32_t)t.tx);
+    q.tx = (int)threadIdx.x - q.ty * t.tx;
+    const int64_t first = (int64_t)q.chunk * (t.ty * t.px) + q.ty;
+    const int cv = q.tile * t.tx + q.tx;
     q.active = q.ty < t.ty && cv < t.cv;
     q.c = (int64_t)cv * V;
+    q.row = q.n * t.P + first;
+    const int64_t left = t.P - first;
+    q.count = left <= 0 ? 0 : left >= (int64_t)t.ty * t.px ? t.px : min(t.px, (int)((uint32_t)(left - 1) / (uint32_t)t.ty) + 1);
     return q;
+}
+
+// Calls fetch(i, r) and body(i, r) for pixels i = 0 ... count - 1; while B of them are worked on the next B are under way.  (All CTAs
+// run at the same time here: without that they wait for memory together and compute together.)
+template <class R, int B, class Fetch, class Body>
+__device__ __forceinline__ void gn_pixels(int count, Fetch fetch, Body body)
+{
+    R r[2][B];
+    const auto load = [&](int i, R (&t)[B]) {
+#pragma unroll
+        for (int k = 0; k < B; ++k)
+            if (i + k < count) fetch(i + k, t[k]);
+    };
+    const auto work = [&](int i, const R (&t)[B]) {
+#pragma unroll
+        for (int k = 0; k < B; ++k)
+            if (i + k < count) body(i + k, t[k]);
+    };
+    load(0, r[0]);
+    for (int i = 0; i < count; i += 2 * B) {
+        load(i + B, r[1]);
+        work(i, r[0]);
+        load(i + 2 * B, r[0]);
+        work(i + B, r[1]);
+    }
 }
 
 template <class E, int V>
@@ -151,60 +198,86 @@ __device__ __forceinline__ float gn_slope(int act, float z)
     }
 }
 
-// Parameters and statistics of V channels from c on, of sample n, and xh = (x - mean) rstd.  fp32 activations: the difference
-// first, which is exact where x is near the mean.  16-bit ones: one multiply-add with mean rstd, off by 2^-24 |mean| rstd where
-// their own rounding is 2^-9 or 2^-12 |x| rstd.
-template <int V, bool ACCURATE>
-struct GnChannels {
-    float mean[V], rstd[V], gamma[V], beta[V];  // not ACCURATE: mean holds -mean rstd
-    __device__ __forceinline__ void load(const GnArgs& a, int64_t n, int64_t c)
-    {
-        const int per = (int)(a.t.C / a.t.G);
-        int g = (int)c / per;
-        int left = (g + 1) * per - (int)c;  // channels until the next group
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            if (left == 0) { ++g; left = per; }
-            --left;
-            mean[j] = a.mean[n * a.t.G + g];
-            rstd[j] = a.rstd[n * a.t.G + g];
-            gamma[j] = a.gamma ? a.gamma[c + j] : 1.f;
-            beta[j] = a.beta ? a.beta[c + j] : 0.f;
-            if constexpr (!ACCURATE) mean[j] = __fmul_rn(-mean[j], rstd[j]);
-        }
-    }
-    __device__ __forceinline__ float xh(float x, int j) const
-    {
-        if constexpr (ACCURATE) return __fmul_rn(__fsub_rn(x, mean[j]), rstd[j]);
-        return __fmaf_rn(x, rstd[j], mean[j]);
-    }
-};
-
-// z = xh gamma + beta of V channels, for the forward pass: one multiply-add more than the difference, or none.
+// V channels from c on of sample n: z = xh gamma + beta as a multiply-add of centre(x), which is x - mean for fp32 activations
+// (a difference that is exact where x is near the mean) and x itself for 16-bit ones, whose own rounding is 2^-9 or 2^-12 |x|
+// against the 2^-24 |mean| that this adds.
 template <int V, bool ACCURATE>
 struct GnAffine {
-    float mean[V], scale[V], shift[V];
+    float mean[ACCURATE ? V : 1], scale[V], shift[V];
     __device__ __forceinline__ void set(int j, float m, float rstd, float gamma, float beta)
     {
-        mean[j] = m;
         scale[j] = __fmul_rn(rstd, gamma);
-        shift[j] = ACCURATE ? beta : __fmaf_rn(-m, scale[j], beta);
+        if constexpr (ACCURATE) {
+            mean[j] = m;
+            shift[j] = beta;
+        } else {
+            shift[j] = __fmaf_rn(-m, scale[j], beta);
+        }
     }
-    __device__ __forceinline__ float z(float x, int j) const
+    __device__ __forceinline__ float centre(float x, int j) const
     {
-        return __fmaf_rn(ACCURATE ? __fsub_rn(x, mean[j]) : x, scale[j], shift[j]);
+        if constexpr (ACCURATE) return __fsub_rn(x, mean[j]);
+        return x;
     }
+    __device__ __forceinline__ float z(float centred, int j) const { return __fmaf_rn(centred, scale[j], shift[j]); }
 };
+// Calls f(j, mean, rstd, group) for V channels from c on of sample n.
+template <int V, class F>
+__device__ __forceinline__ void gn_channels(const GnArgs& a, int64_t n, int64_t c, F f)
+{
+    const int per = (int)(a.t.C / a.t.G);
+    int g = (int)c / per;
+    int left = (g + 1) * per - (int)c;  // channels until the next group
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (left == 0) { ++g; left = per; }
+        --left;
+        const int64_t at = n * a.t.G + g;
+        f(j, __ldcg(a.mean + at), __ldcg(a.rstd + at), at);
+    }
+}
+template <int V, bool ACCURATE>
+__device__ __forceinline__ void gn_affine(const GnArgs& a, int64_t n, int64_t c, GnAffine<V, ACCURATE>& f)
+{
+    gn_channels<V>(a, n, c, [&](int j, float mean, float rstd, int64_t) {
+        f.set(j, mean, rstd, a.gamma ? a.gamma[c + j] : 1.f, a.beta ? a.beta[c + j] : 0.f);
+    });
+}
+// dx = dz scale + centre(x) slope + offset, from the group's means of gamma dz and gamma dz xh.
+template <bool ACCURATE>
+__device__ __forceinline__ void gn_gradient_terms(float2 means, float mean, float rstd, float& slope, float& offset)
+{
+    slope = -__fmul_rn(__fmul_rn(rstd, rstd), means.y);
+    offset = -__fmul_rn(rstd, means.x);
+    if constexpr (!ACCURATE) offset = __fmaf_rn(-mean, slope, offset);
+}
+// Sum of dz xh from the sums of dz and of dz centre(x).
+template <bool ACCURATE>
+__device__ __forceinline__ float gn_gamma_sum(float dz, float dzx, float mean, float rstd)
+{
+    return __fmul_rn(rstd, ACCURATE ? dzx : __fmaf_rn(-mean, dz, dzx));
+}
 
 // V elements as they lie in memory.
 template <class E, int V> struct GnRaw { E e; };
 template <class E> struct GnRaw<E, 8> { Raw8<E> e; };
+// (volatile: the compiler otherwise moves a load that was asked for early back to where its value is needed)
+__device__ __forceinline__ uint4 gn_load16(const void* p)
+{
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
 template <class E, int V>
 __device__ __forceinline__ GnRaw<E, V> gn_fetch(const E* p)
 {
     GnRaw<E, V> r;
-    if constexpr (V == 8) r.e = load_raw8(p);
-    else r.e = *p;
+    if constexpr (V == 8) {
+        r.e.a = gn_load16(p);
+        if constexpr (sizeof(E) == 4) r.e.b = gn_load16(p + 4);
+    } else {
+        r.e = *p;
+    }
     return r;
 }
 template <class E, int V>
@@ -217,12 +290,16 @@ __device__ __forceinline__ void gn_open(const GnRaw<E, V>& r, float (&v)[V])
 template <int V> struct GnKept { int8_t c; uint32_t s; };
 template <> struct GnKept<8> { uint2 c; uint32_t s; };
 template <int V>
-__device__ __forceinline__ GnKept<V> gn_fetch_kept(const int8_t* codes, const uint8_t* scales, int64_t row, int64_t C, int64_t groups, int64_t c)
+__device__ __forceinline__ GnKept<V> gn_fetch_kept(const int8_t* code, const uint8_t* scale)
 {
     GnKept<V> r;
-    if constexpr (V == 8) r.c = *reinterpret_cast<const uint2*>(codes + row * C + c);
-    else r.c = codes[row * C + c];
-    r.s = scales[row * groups + c / kAct8Group];
+    if constexpr (V == 8) {
+        asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(r.c.x), "=r"(r.c.y) : "l"(code));
+        asm volatile("ld.global.u8 %0, [%1];" : "=r"(r.s) : "l"(scale));
+    } else {
+        r.c = *code;
+        r.s = *scale;
+    }
     return r;
 }
 template <int V>

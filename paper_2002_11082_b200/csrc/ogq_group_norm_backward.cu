@@ -13,23 +13,44 @@ template <class E, int V, bool KEPT>
 struct GnPair {
     GnRaw<E, V> dy;
     std::conditional_t<KEPT, GnKept<V>, GnRaw<E, V>> x;
-    __device__ __forceinline__ void fetch(const GnArgs& a, int64_t row, int64_t c, int64_t groups)
-    {
-        dy = gn_fetch<E, V>((const E*)a.dy + row * a.t.C + c);
-        if constexpr (KEPT) x = gn_fetch_kept<V>(a.codes, a.scales, row, a.t.C, groups, c);
-        else x = gn_fetch<E, V>((const E*)a.x + row * a.t.C + c);
-    }
+    // dz, and x less the mean or as it is
     template <int ACT, bool ACCURATE>
-    __device__ __forceinline__ void open(int act, const GnChannels<V, ACCURATE>& ch, float (&dz)[V], float (&xh)[V]) const
+    __device__ __forceinline__ void open(int act, const GnAffine<V, ACCURATE>& f, float (&dz)[V], float (&xc)[V]) const
     {
         gn_open<E, V>(dy, dz);
-        if constexpr (KEPT) gn_open<V>(x, xh);
-        else gn_open<E, V>(x, xh);
+        if constexpr (KEPT) gn_open<V>(x, xc);
+        else gn_open<E, V>(x, xc);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            xh[j] = ch.xh(xh[j], j);
-            dz[j] = __fmul_rn(dz[j], gn_slope<ACT, ACCURATE>(act, __fmaf_rn(xh[j], ch.gamma[j], ch.beta[j])));
+            xc[j] = f.centre(xc[j], j);
+            dz[j] = __fmul_rn(dz[j], gn_slope<ACT, ACCURATE>(act, f.z(xc[j], j)));
         }
+    }
+};
+
+// The pointers of a thread's first pixel and how far the next one's are.
+template <class E, int V, bool KEPT>
+struct GnReader {
+    const E *dy, *x;
+    const int8_t* codes;
+    const uint8_t* scales;
+    int step, scale_step;
+    __device__ __forceinline__ GnReader(const GnArgs& a, const GnPlace& q)
+    {
+        const int groups = (int)act8_groups(a.t.C);
+        const int64_t at = q.row * a.t.C + q.c;
+        dy = (const E*)a.dy + at;
+        x = KEPT ? nullptr : (const E*)a.x + at;
+        codes = KEPT ? a.codes + at : nullptr;
+        scales = KEPT ? a.scales + q.row * groups + (uint32_t)q.c / kAct8Group : nullptr;
+        step = a.t.ty * (int)a.t.C;
+        scale_step = a.t.ty * groups;
+    }
+    __device__ __forceinline__ void fetch(int i, GnPair<E, V, KEPT>& r) const
+    {
+        r.dy = gn_fetch<E, V>(dy + (int64_t)i * step);
+        if constexpr (KEPT) r.x = gn_fetch_kept<V>(codes + (int64_t)i * step, scales + (int64_t)i * scale_step);
+        else r.x = gn_fetch<E, V>(x + (int64_t)i * step);
     }
 };
 
@@ -41,37 +62,30 @@ __global__ void __launch_bounds__(kThreads) k_gn_grad_sums(const __grid_constant
     constexpr bool kAccurate = sizeof(E) == 4;
     __shared__ float2 sh[kThreads * V];
     const GnPlace q = gn_place<V>(a.t);
-    const int64_t groups = act8_groups(a.t.C);
     if (q.active) {
-        GnChannels<V, kAccurate> ch;
-        ch.load(a, q.n, q.c);
+        const GnReader<E, V, KEPT> in(a, q);
+        GnAffine<V, kAccurate> f;
+        gn_affine(a, q.n, q.c, f);
         float sb[V], sg[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) sb[j] = sg[j] = 0.f;
-        for (int64_t p = q.first; p < q.last; p += kGnBatch * a.t.ty) {
-            GnPair<E, V, KEPT> r[kGnBatch];
+        gn_pixels<GnPair<E, V, KEPT>, 1>(q.count, [&](int i, GnPair<E, V, KEPT>& r) { in.fetch(i, r); },
+                                      [&](int, const GnPair<E, V, KEPT>& r) {
+                                          float dz[V], xc[V];
+                                          r.template open<ACT, kAccurate>(a.act, f, dz, xc);
 #pragma unroll
-            for (int k = 0; k < kGnBatch; ++k)
-                if (p + k * a.t.ty < q.last) r[k].fetch(a, q.n * a.t.P + p + k * a.t.ty, q.c, groups);
-#pragma unroll
-            for (int k = 0; k < kGnBatch; ++k) {
-                if (p + k * a.t.ty >= q.last) break;
-                float dz[V], xh[V];
-                r[k].template open<ACT, kAccurate>(a.act, ch, dz, xh);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    sb[j] = __fadd_rn(sb[j], dz[j]);
-                    sg[j] = __fmaf_rn(dz[j], xh[j], sg[j]);
-                }
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) sh[(q.ty * a.t.tx + q.tx) * V + j] = make_float2(sb[j], sg[j]);
+                                          for (int j = 0; j < V; ++j) {
+                                              sb[j] = __fadd_rn(sb[j], dz[j]);
+                                              sg[j] = __fmaf_rn(dz[j], xc[j], sg[j]);
+                                          }
+                                      });
+        gn_channels<V>(a, q.n, q.c, [&](int j, float mean, float rstd, int64_t) {
+            sh[(q.ty * a.t.tx + q.tx) * V + j] = make_float2(sb[j], gn_gamma_sum<kAccurate>(sb[j], sg[j], mean, rstd));
+        });
     }
     __syncthreads();
-    const int tile = (int)(blockIdx.x % (unsigned)a.t.ctiles);
     for (int j = threadIdx.x; j < a.t.tx * V; j += kThreads) {
-        const int64_t c = (int64_t)tile * a.t.tx * V + j;
+        const int64_t c = (int64_t)q.tile * a.t.tx * V + j;
         if (c >= a.t.C) break;
         float2 s = make_float2(0.f, 0.f);
         for (int y = 0; y < a.t.ty; ++y) {
@@ -79,7 +93,7 @@ __global__ void __launch_bounds__(kThreads) k_gn_grad_sums(const __grid_constant
             s.x += e.x;
             s.y += e.y;
         }
-        a.part[(q.n * a.t.chunks + q.chunk) * a.t.C + c] = s;
+        a.part[((int64_t)q.n * a.t.chunks + q.chunk) * a.t.C + c] = s;
     }
 }
 
@@ -155,33 +169,22 @@ __global__ void __launch_bounds__(kThreads) k_gn_grad(const __grid_constant__ Gn
     constexpr bool kAccurate = sizeof(E) == 4;
     const GnPlace q = gn_place<V>(a.t);
     if (!q.active) return;
-    const int64_t groups = act8_groups(a.t.C);
-    GnChannels<V, kAccurate> ch;
-    ch.load(a, q.n, q.c);
-    float c0[V], c1[V], c2[V];  // dx = dz c1 - xh c2 - c0
-    const int per = (int)(a.t.C / a.t.G);
+    const GnReader<E, V, KEPT> in(a, q);
+    GnAffine<V, kAccurate> f;
+    gn_affine(a, q.n, q.c, f);
+    float slope[V], offset[V];
+    gn_channels<V>(a, q.n, q.c, [&](int j, float mean, float rstd, int64_t at) {
+        gn_gradient_terms<kAccurate>(__ldcg(a.sums + at), mean, rstd, slope[j], offset[j]);
+    });
+    E* out = (E*)a.out + q.row * a.t.C + q.c;
+    gn_pixels<GnPair<E, V, KEPT>, sizeof(E) == 2 ? 2 : 1>(q.count, [&](int i, GnPair<E, V, KEPT>& r) { in.fetch(i, r); },
+                                  [&](int i, const GnPair<E, V, KEPT>& r) {
+                                      float dz[V], xc[V];
+                                      r.template open<ACT, kAccurate>(a.act, f, dz, xc);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const float2 s = __ldcg(a.sums + q.n * a.t.G + ((int)q.c + j) / per);
-        c0[j] = __fmul_rn(-s.x, ch.rstd[j]);
-        c1[j] = __fmul_rn(ch.gamma[j], ch.rstd[j]);
-        c2[j] = __fmul_rn(-s.y, ch.rstd[j]);
-    }
-    for (int64_t p = q.first; p < q.last; p += kGnBatch * a.t.ty) {
-        GnPair<E, V, KEPT> r[kGnBatch];
-#pragma unroll
-        for (int k = 0; k < kGnBatch; ++k)
-            if (p + k * a.t.ty < q.last) r[k].fetch(a, q.n * a.t.P + p + k * a.t.ty, q.c, groups);
-#pragma unroll
-        for (int k = 0; k < kGnBatch; ++k) {
-            if (p + k * a.t.ty >= q.last) break;
-            float dz[V], xh[V];
-            r[k].template open<ACT, kAccurate>(a.act, ch, dz, xh);
-#pragma unroll
-            for (int j = 0; j < V; ++j) dz[j] = __fmaf_rn(dz[j], c1[j], __fmaf_rn(xh[j], c2[j], c0[j]));
-            gn_store((E*)a.out + (q.n * a.t.P + p + k * a.t.ty) * a.t.C + q.c, dz);
-        }
-    }
+                                      for (int j = 0; j < V; ++j) dz[j] = __fmaf_rn(dz[j], f.scale[j], __fmaf_rn(xc[j], slope[j], offset[j]));
+                                      gn_store(out + (int64_t)i * in.step, dz);
+                                  });
 }
 
 // The whole pass of one slab (see ogq_group_norm_resident.cuh): dy and x are read once, dz stays in fp32 registers (its slope costs
@@ -218,8 +221,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_gn_backward(const __grid_consta
             rx[u] = in[u] ? load_raw8((const E*)a.x + row * a.t.C + q.c) : zero_raw8<E>();
         }
     }
-    GnChannels<8, kAccurate> ch;
-    if (q.active) ch.load(a, q.n, q.c);
+    GnAffine<8, kAccurate> z;
+    if (q.active) gn_affine(a, q.n, q.c, z);
     float dz[U][8];
     float2 sum[8];
 #pragma unroll
@@ -232,14 +235,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_gn_backward(const __grid_consta
         else unpack8(rx[u], f);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float xh = ch.xh(f[j], j);
-            dz[u][j] = __fmul_rn(dz[u][j], act_slope<ACT, kAccurate>(__fmaf_rn(xh, ch.gamma[j], ch.beta[j])));
+            const float xc = z.centre(f[j], j);
+            dz[u][j] = __fmul_rn(dz[u][j], act_slope<ACT, kAccurate>(z.z(xc, j)));
             if (in[u]) {
                 sum[j].x = __fadd_rn(sum[j].x, dz[u][j]);
-                sum[j].y = __fmaf_rn(dz[u][j], xh, sum[j].y);
+                sum[j].y = __fmaf_rn(dz[u][j], xc, sum[j].y);
             }
         }
     }
+    if (q.active)
+        gn_channels<8>(a, q.n, q.c, [&](int j, float mean, float rstd, int64_t) {
+            sum[j].y = gn_gamma_sum<kAccurate>(sum[j].x, sum[j].y, mean, rstd);
+        });
     gn_put_sums(s, q, sum, sh, s.width);
     __syncthreads();
     for (int c = threadIdx.x; c < s.width; c += kThreads) {
@@ -290,14 +297,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_gn_backward(const __grid_consta
     }
     __syncthreads();
     if (q.active) {
-        float2 g[8];
-        int k = q.c0 / s.per, left = (k + 1) * s.per - q.c0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (left == 0) { ++k; left = s.per; }
-            --left;
-            g[j] = sh_group[k];
-        }
+        float slope[8], offset[8];
+        const int64_t base = q.n * a.t.G + (int)(q.c - q.c0) / s.per;  // the slab's first group
+        gn_channels<8>(a, q.n, q.c, [&](int j, float mean, float rstd, int64_t at) {
+            gn_gradient_terms<kAccurate>(sh_group[at - base], mean, rstd, slope[j], offset[j]);
+        });
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (!in[u]) continue;
@@ -306,10 +310,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_gn_backward(const __grid_consta
             if constexpr (KEPT) act8_values(kx[u], act8_unit(ks[u]), f);
             else unpack8(rx[u], f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float xh = ch.xh(f[j], j);
-                f[j] = __fmul_rn(ch.rstd[j], __fmaf_rn(-xh, g[j].y, __fmaf_rn(dz[u][j], ch.gamma[j], -g[j].x)));
-            }
+            for (int j = 0; j < 8; ++j) f[j] = __fmaf_rn(dz[u][j], z.scale[j], __fmaf_rn(z.centre(f[j], j), slope[j], offset[j]));
             store8((E*)a.out + row * a.t.C + q.c, f);
         }
     }
@@ -325,7 +326,7 @@ cudaError_t launch_group_norm_backward(const GroupNorm& p, int sm_count, cudaStr
     const bool kept = p.codes != nullptr;
     const bool vec = p.C % 8 == 0 && gn_aligned(p.dy, 16) && gn_aligned(p.out, 16) && (p.C * size) % 16 == 0 &&
                      (kept ? gn_aligned(p.codes, 8) : gn_aligned(p.x, 16));
-    GnArgs a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, vec ? 8 : 1, sm_count));
+    GnArgs a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, vec ? 8 : 1, sm_count, 1));
     const int channel_ctas = p.dgamma || p.dbeta ? (int)((p.C + 7) / 8) : 0;
     GnSlab slab;
     if (vec && a.t.ctas > 0) {
@@ -356,38 +357,40 @@ cudaError_t launch_group_norm_backward(const GroupNorm& p, int sm_count, cudaStr
             return e;
         }
     }
+    if (a.t.ctas > 0x7fffffff) return cudaErrorInvalidValue;
     const auto launch = [&](auto which) {
         constexpr bool kSums = decltype(which)::value;
+        const auto one = [&](auto kernel, int V) {
+            a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, V, gn_wave(kernel, sm_count), kSums ? kGnMinPx : kGnMinPxApply));
+            if (a.t.ctas == 0) return cudaSuccess;
+            launch_begin(kSums ? "k_gn_grad_sums" : "k_gn_grad", stream);
+            const cudaError_t r = launch_pdl(kernel, (int)a.t.ctas, kThreads, 0, stream, a);
+            launch_end(stream);
+            return r;
+        };
         return with_dtype(p.dtype, [&](auto elem) {
             using E = decltype(elem);
             return with_bool(kept, [&](auto k) {
                 constexpr bool K = decltype(k)::value;
-                if (!vec) return launch_pdl(kSums ? k_gn_grad_sums<E, 1, -1, K> : k_gn_grad<E, 1, -1, K>, (int)a.t.ctas, kThreads, 0, stream, a);
+                if (!vec) return one(kSums ? k_gn_grad_sums<E, 1, -1, K> : k_gn_grad<E, 1, -1, K>, 1);
                 return with_act(p.act, [&](auto act) {
                     constexpr int A = decltype(act)::value;
-                    return launch_pdl(kSums ? k_gn_grad_sums<E, 8, A, K> : k_gn_grad<E, 8, A, K>, (int)a.t.ctas, kThreads, 0, stream, a);
+                    return one(kSums ? k_gn_grad_sums<E, 8, A, K> : k_gn_grad<E, 8, A, K>, 8);
                 });
             });
         });
     };
-    cudaError_t e = cudaSuccess;
-    if (a.t.ctas > 0) {
-        launch_begin("k_gn_grad_sums", stream);
-        e = launch(std::true_type{});
-        launch_end(stream);
-        if (e != cudaSuccess) return e;
-    }
-    const int group_ctas = a.t.ctas > 0 ? (int)(p.N * p.G) : 0;
+    const bool any = a.t.ctas > 0;
+    cudaError_t e = launch(std::true_type{});
+    if (e != cudaSuccess) return e;
+    const int group_ctas = any ? (int)(p.N * p.G) : 0;
     if (group_ctas + channel_ctas > 0) {
         launch_begin("k_gn_grad_join", stream);
         e = launch_pdl(k_gn_grad_join, group_ctas + channel_ctas, kThreads, 0, stream, a, group_ctas);
         launch_end(stream);
     }
-    if (e != cudaSuccess || a.t.ctas == 0) return e;
-    launch_begin("k_gn_grad", stream);
-    e = launch(std::false_type{});
-    launch_end(stream);
-    return e;
+    if (e != cudaSuccess || !any) return e;
+    return launch(std::false_type{});
 }
 
 }  // namespace ogq

@@ -16,59 +16,53 @@ __global__ void __launch_bounds__(kThreads) k_gn_moments(const __grid_constant__
     pdl_launch_dependents();
     __shared__ float2 sh[kThreads * V];
     const GnPlace q = gn_place<V>(a.t);
-    float shift[V], s1[V], s2[V];
-    int n = 0;
     if (q.active) {
-        const E* x = (const E*)a.x + q.n * a.t.P * a.t.C + q.c;
+        const E* x = (const E*)a.x + q.row * a.t.C + q.c;
+        const int step = a.t.ty * (int)a.t.C;
+        float shift[V], s1[V], s2[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) s1[j] = s2[j] = shift[j] = 0.f;
-        for (int64_t p = q.first; p < q.last; p += kGnBatch * a.t.ty) {
-            GnRaw<E, V> r[kGnBatch];
+        gn_pixels<GnRaw<E, V>, 2>(q.count, [&](int i, GnRaw<E, V>& r) { r = gn_fetch<E, V>(x + (int64_t)i * step); },
+                               [&](int i, const GnRaw<E, V>& r) {
+                                   float v[V];
+                                   gn_open<E, V>(r, v);
+                                   if (i == 0) {
 #pragma unroll
-            for (int k = 0; k < kGnBatch; ++k)
-                if (p + k * a.t.ty < q.last) r[k] = gn_fetch<E, V>(x + (p + k * a.t.ty) * a.t.C);
+                                       for (int j = 0; j < V; ++j) shift[j] = v[j];
+                                   }
 #pragma unroll
-            for (int k = 0; k < kGnBatch; ++k) {
-                if (p + k * a.t.ty >= q.last) break;
-                float v[V];
-                gn_open<E, V>(r[k], v);
-                if (k == 0 && n == 0) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) shift[j] = v[j];
-                }
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float d = __fsub_rn(v[j], shift[j]);
-                    s1[j] = __fadd_rn(s1[j], d);
-                    s2[j] = __fmaf_rn(d, d, s2[j]);
-                }
-                ++n;
-            }
-        }
+                                   for (int j = 0; j < V; ++j) {
+                                       const float d = __fsub_rn(v[j], shift[j]);
+                                       s1[j] = __fadd_rn(s1[j], d);
+                                       s2[j] = __fmaf_rn(d, d, s2[j]);
+                                   }
+                               });
+        const float inv = q.count > 0 ? 1.f / (float)q.count : 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float m = n ? s1[j] / (float)n : 0.f;
+            const float m = __fmul_rn(s1[j], inv);
             sh[(q.ty * a.t.tx + q.tx) * V + j] = make_float2(shift[j] + m, fmaxf(__fmaf_rn(-m, s1[j], s2[j]), 0.f));
         }
     }
     __syncthreads();
     // pixels of the rows of threads: row y has `whole` and, if y < more, one more
     const int64_t begin = (int64_t)q.chunk * a.t.ty * a.t.px;
-    const int count = (int)(q.last - begin), whole = count / a.t.ty, more = count - whole * a.t.ty;
-    const int tile = (int)(blockIdx.x % (unsigned)a.t.ctiles);
+    const int count = (int)(a.t.P - begin < (int64_t)a.t.ty * a.t.px ? a.t.P - begin : (int64_t)a.t.ty * a.t.px);
+    const int whole = (int)((uint32_t)count / (uint32_t)a.t.ty), more = count - whole * a.t.ty;
+    const float inv = 1.f / (float)count, w0 = (float)whole, w1 = (float)(whole + 1);
     for (int j = threadIdx.x; j < a.t.tx * V; j += kThreads) {
-        const int64_t c = (int64_t)tile * a.t.tx * V + j;
+        const int64_t c = (int64_t)q.tile * a.t.tx * V + j;
         if (c >= a.t.C) break;
         float sum = 0.f;
-        for (int y = 0; y < a.t.ty; ++y) sum += (float)(whole + (y < more)) * sh[y * a.t.tx * V + j].x;
-        const float mean = sum / (float)count;
+        for (int y = 0; y < a.t.ty; ++y) sum = __fmaf_rn(y < more ? w1 : w0, whole || y < more ? sh[y * a.t.tx * V + j].x : 0.f, sum);
+        const float mean = __fmul_rn(sum, inv);
         float m2 = 0.f;
         for (int y = 0; y < a.t.ty; ++y) {
             const float2 e = sh[y * a.t.tx * V + j];
-            const float d = e.x - mean, w = (float)(whole + (y < more));
-            m2 += w > 0.f ? __fmaf_rn(w * d, d, e.y) : 0.f;
+            const float d = e.x - mean;
+            if (whole || y < more) m2 += __fmaf_rn((y < more ? w1 : w0) * d, d, e.y);
         }
-        a.part[(q.n * a.t.chunks + q.chunk) * a.t.C + c] = make_float2(mean, m2);
+        a.part[((int64_t)q.n * a.t.chunks + q.chunk) * a.t.C + c] = make_float2(mean, m2);
     }
 }
 
@@ -146,42 +140,30 @@ __global__ void __launch_bounds__(kThreads) k_gn_apply(const __grid_constant__ G
     const GnPlace q = gn_place<V>(a.t);
     if (!q.active) return;  // KEEP: whole groups of lanes, since tx is a multiple of 4
     GnAffine<V, kAccurate> f;
-    {
-        const int per = (int)(a.t.C / a.t.G);
-        int g = (int)q.c / per, left = (g + 1) * per - (int)q.c;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            if (left == 0) { ++g; left = per; }
-            --left;
-            const int64_t at = q.n * a.t.G + g;
-            f.set(j, __ldcg(a.mean + at), __ldcg(a.rstd + at), a.gamma ? a.gamma[q.c + j] : 1.f, a.beta ? a.beta[q.c + j] : 0.f);
-        }
-    }
+    gn_affine(a, q.n, q.c, f);
     const unsigned team = 0xfu << (threadIdx.x & 28);
-    for (int64_t p = q.first; p < q.last; p += kGnBatch * a.t.ty) {
-        const int64_t at = (q.n * a.t.P + p) * a.t.C + q.c, step = a.t.ty * a.t.C;
-        GnRaw<E, V> r[kGnBatch];
+    const int64_t at = q.row * a.t.C + q.c;
+    const int step = a.t.ty * (int)a.t.C;
+    const E* x = (const E*)a.x + at;
+    E* out = (E*)a.out + at;
+    gn_pixels<GnRaw<E, V>, 2>(q.count, [&](int i, GnRaw<E, V>& r) { r = gn_fetch<E, V>(x + (int64_t)i * step); },
+                           [&](int i, const GnRaw<E, V>& r) {
+                               float v[V], y[V];
+                               gn_open<E, V>(r, v);
+                               const int64_t by = (int64_t)i * step;
+                               if constexpr (KEEP != 0 && V == 8) {
+                                   uint32_t b = max_abs_bits(r.e);
+                                   b = max(b, __shfl_xor_sync(team, b, 1));
+                                   b = max(b, __shfl_xor_sync(team, b, 2));
+                                   const uint32_t byte = act8_byte(b);
+                                   *reinterpret_cast<uint2*>(a.codes + at + by) =
+                                       act8_codes<KEEP == 2>(v, byte, (uint64_t)(at + by), 0u, a.stream_id, a.keys);
+                                   if ((threadIdx.x & 3) == 0) a.scales[(uint64_t)(at + by) / kAct8Group] = (uint8_t)byte;
+                               }
 #pragma unroll
-        for (int k = 0; k < kGnBatch; ++k)
-            if (p + k * a.t.ty < q.last) r[k] = gn_fetch<E, V>((const E*)a.x + at + k * step);
-#pragma unroll
-        for (int k = 0; k < kGnBatch; ++k) {
-            if (p + k * a.t.ty >= q.last) break;
-            float v[V], y[V];
-            gn_open<E, V>(r[k], v);
-#pragma unroll
-            for (int j = 0; j < V; ++j) y[j] = gn_value<ACT, kAccurate>(a.act, f.z(v[j], j));
-            if constexpr (KEEP != 0 && V == 8) {
-                uint32_t b = max_abs_bits(v);
-                b = max(b, __shfl_xor_sync(team, b, 1));
-                b = max(b, __shfl_xor_sync(team, b, 2));
-                const uint32_t byte = act8_byte(b);
-                *reinterpret_cast<uint2*>(a.codes + at + k * step) = act8_codes<KEEP == 2>(v, byte, (uint64_t)(at + k * step), 0u, a.stream_id, a.keys);
-                if ((threadIdx.x & 3) == 0) a.scales[(at + k * step) / kAct8Group] = (uint8_t)byte;
-            }
-            gn_store((E*)a.out + at + k * step, y);
-        }
-    }
+                               for (int j = 0; j < V; ++j) y[j] = gn_value<ACT, kAccurate>(a.act, f.z(f.centre(v[j], j), j));
+                               gn_store(out + by, y);
+                           });
 }
 
 // The whole pass of one slab (see ogq_group_norm_resident.cuh): x is read once.  The CTA's mean and its sum of squares about that
@@ -312,18 +294,18 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : 3) k_gn_forward(const _
             float f[8], y[8];
             unpack8(v[u], f);
             if constexpr (KEEP != 0) {  // four lanes hold a group of 32 channels; the same pixel, so all four are in or none is
-                uint32_t b = max_abs_bits(f);
+                uint32_t b = max_abs_bits(v[u]);
                 b = max(b, __shfl_xor_sync(team, b, 1));
                 b = max(b, __shfl_xor_sync(team, b, 2));
                 const uint32_t byte = act8_byte(b);
                 if (in[u]) {
                     *reinterpret_cast<uint2*>(a.codes + row * a.t.C + q.c) =
                         act8_codes<KEEP == 2>(f, byte, (uint64_t)(row * a.t.C + q.c), 0u, a.stream_id, a.keys);
-                    if ((threadIdx.x & 3) == 0) a.scales[(row * a.t.C + q.c) / kAct8Group] = (uint8_t)byte;
+                    if ((threadIdx.x & 3) == 0) a.scales[(uint64_t)(row * a.t.C + q.c) / kAct8Group] = (uint8_t)byte;
                 }
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = act_value<ACT, kAccurate>(z.z(f[j], j));
+            for (int j = 0; j < 8; ++j) y[j] = act_value<ACT, kAccurate>(z.z(z.centre(f[j], j), j));
             if (in[u]) store8((E*)a.out + row * a.t.C + q.c, y);
         }
     }
@@ -352,7 +334,7 @@ cudaError_t launch_group_norm_forward(const GroupNorm& p, int sm_count, cudaStre
         if (gn_slab(p.N, p.P, p.C, p.G, (int)size, fused, 2, slab) && slab.ctas <= (int64_t)sm_count * kGnFewCtas) u = 2;
         else if (getenv("GN_MOST") && gn_slab(p.N, p.P, p.C, p.G, (int)size, fused, most, slab)) u = most;
         if (u) {
-            const GnArgs a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, 8, sm_count));
+            const GnArgs a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, 8, sm_count, 1));
             launch_begin("k_gn_forward", stream);
             const cudaError_t e = with_dtype(p.dtype, [&](auto elem) {
                 using E = decltype(elem);
@@ -380,34 +362,36 @@ cudaError_t launch_group_norm_forward(const GroupNorm& p, int sm_count, cudaStre
         e = launch_act8_forward(f, sm_count, stream);
         if (e != cudaSuccess) return e;
     }
-    const GnArgs a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, vec ? 8 : 1, sm_count));
-    if (a.t.ctas > 0) {
-        launch_begin("k_gn_moments", stream);
-        e = with_dtype(p.dtype, [&](auto elem) {
-            using E = decltype(elem);
-            return vec ? launch_pdl(k_gn_moments<E, 8>, (int)a.t.ctas, kThreads, 0, stream, a)
-                       : launch_pdl(k_gn_moments<E, 1>, (int)a.t.ctas, kThreads, 0, stream, a);
-        });
+    const auto launch = [&](const char* name, auto kernel, int V, int least, GnArgs& a) {
+        a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, V, gn_wave(kernel, sm_count), least));
+        if (a.t.ctas == 0) return cudaSuccess;
+        if (a.t.ctas > 0x7fffffff) return cudaErrorInvalidValue;
+        launch_begin(name, stream);
+        const cudaError_t r = launch_pdl(kernel, (int)a.t.ctas, kThreads, 0, stream, a);
         launch_end(stream);
-        if (e != cudaSuccess) return e;
-    }
-    launch_begin("k_gn_stats", stream);
-    e = launch_pdl(k_gn_stats, (int)(p.N * p.G), kThreads, 0, stream, a);
-    launch_end(stream);
-    if (e != cudaSuccess || a.t.ctas == 0) return e;
-    launch_begin("k_gn_apply", stream);
+        return r;
+    };
+    GnArgs sums;
     e = with_dtype(p.dtype, [&](auto elem) {
         using E = decltype(elem);
-        if (!vec) return launch_pdl(k_gn_apply<E, 1, -1, 0>, (int)a.t.ctas, kThreads, 0, stream, a);
+        return vec ? launch("k_gn_moments", k_gn_moments<E, 8>, 8, kGnMinPx, sums) : launch("k_gn_moments", k_gn_moments<E, 1>, 1, kGnMinPx, sums);
+    });
+    if (e != cudaSuccess) return e;
+    launch_begin("k_gn_stats", stream);
+    e = launch_pdl(k_gn_stats, (int)(p.N * p.G), kThreads, 0, stream, sums);
+    launch_end(stream);
+    if (e != cudaSuccess) return e;
+    return with_dtype(p.dtype, [&](auto elem) {
+        using E = decltype(elem);
+        GnArgs a;
+        if (!vec) return launch("k_gn_apply", k_gn_apply<E, 1, -1, 0>, 1, kGnMinPxApply, a);
         return with_act(p.act, [&](auto act) {
             constexpr int A = decltype(act)::value;
-            if (!fused) return launch_pdl(k_gn_apply<E, 8, A, 0>, (int)a.t.ctas, kThreads, 0, stream, a);
-            if (p.rounding == OGQ_ROUND_RANDOM) return launch_pdl(k_gn_apply<E, 8, A, 2>, (int)a.t.ctas, kThreads, 0, stream, a);
-            return launch_pdl(k_gn_apply<E, 8, A, 1>, (int)a.t.ctas, kThreads, 0, stream, a);
+            if (!fused) return launch("k_gn_apply", k_gn_apply<E, 8, A, 0>, 8, kGnMinPxApply, a);
+            if (p.rounding == OGQ_ROUND_RANDOM) return launch("k_gn_apply", k_gn_apply<E, 8, A, 2>, 8, kGnMinPxApply, a);
+            return launch("k_gn_apply", k_gn_apply<E, 8, A, 1>, 8, kGnMinPxApply, a);
         });
     });
-    launch_end(stream);
-    return e;
 }
 
 }  // namespace ogq
