@@ -17,11 +17,11 @@ struct GnTiles {
     int64_t ctas;
 };
 
-constexpr int kGnMinPx = 16, kGnMaxPx = 64;  // pixels a thread where sums are taken: those in fp32 stay short, partial sums stay few
-constexpr int kGnMinPxApply = 4;             // where not
+constexpr int kGnMaxPx = 64;                 // pixels a thread, at most: sums in fp32 stay short
+constexpr int kGnMinChunk = 16;              // pixels of a chunk whose sums are kept, at least: partial sums stay few
 
 // Tiles for a kernel of which `wave` CTAs run at a time: whole waves, as near as the sizes allow (25.7 M bf16 values, moments: 800
-// CTAs on 592 places took 19 us, 576 take 12), of at least `least` pixels a thread.
+// CTAs on 592 places took 19 us, 576 take 12), of at least `least` pixels a chunk and two a thread.
 inline GnTiles gn_tiles(int64_t N, int64_t P, int64_t C, int64_t G, int V, int64_t wave, int least)
 {
     GnTiles t;
@@ -40,7 +40,8 @@ inline GnTiles gn_tiles(int64_t N, int64_t P, int64_t C, int64_t G, int V, int64
             if (q <= kGnMaxPx) { px = q; break; }
         }
     }
-    t.px = (int)(px < least ? least : px);
+    const int64_t lower = (least + t.ty - 1) / t.ty < 2 ? 2 : (least + t.ty - 1) / t.ty;
+    t.px = (int)(px < lower ? lower : px);
     t.chunks = (int)((units + t.px - 1) / t.px);
     t.ctas = tasks * t.chunks;
     return t;
@@ -62,9 +63,7 @@ struct GnWs {
 };
 inline size_t gn_part_bytes(int64_t N, int64_t P, int64_t C)
 {
-    const int64_t tx = C < kThreads ? C : kThreads, ty = kThreads / tx;  // single channels have the most chunks (vectors have larger ty)
-    const int64_t chunks = (P + ty * kGnMinPx - 1) / (ty * kGnMinPx);
-    return (size_t)(N * chunks * C) * sizeof(float2);
+    return (size_t)(N * ((P + kGnMinChunk - 1) / kGnMinChunk) * C) * sizeof(float2);
 }
 inline GnWs gn_ws(void* ws, int64_t N, int64_t G)
 {
@@ -233,7 +232,7 @@ __device__ __forceinline__ void gn_channels(const GnArgs& a, int64_t n, int64_t 
         if (left == 0) { ++g; left = per; }
         --left;
         const int64_t at = n * a.t.G + g;
-        f(j, __ldcg(a.mean + at), __ldcg(a.rstd + at), at);
+        f(j, a.mean[at], a.rstd[at], at);  // (from L1 where they are asked for again)
     }
 }
 template <int V, bool ACCURATE>

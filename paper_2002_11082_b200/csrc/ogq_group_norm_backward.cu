@@ -3,7 +3,6 @@
 //   dx = rstd (gamma dz - m1 - xh m2),  m1, m2 = means over the group of gamma dz and gamma dz xh,
 // which are sums over the group's channels of gamma times the channel's two sums.
 // Any shape in three steps: both sums per channel of a chunk of pixels; joined per group and over the samples; the elements.
-#include <stdlib.h>
 #include "ogq_group_norm_resident.cuh"
 
 namespace ogq {
@@ -190,7 +189,7 @@ __global__ void __launch_bounds__(kThreads) k_gn_grad(const __grid_constant__ Gn
 // The whole pass of one slab (see ogq_group_norm_resident.cuh): dy and x are read once, dz stays in fp32 registers (its slope costs
 // more than its 8 registers a vector), xh is computed again from x.
 template <class E, int ACT, bool KEPT, int U>
-__global__ void __launch_bounds__(kThreads, 2) k_gn_backward(const __grid_constant__ GnArgs a, const __grid_constant__ GnSlab s)
+__global__ void __launch_bounds__(kThreads, U <= 2 ? 3 : 2) k_gn_backward(const __grid_constant__ GnArgs a, const __grid_constant__ GnSlab s)
 {
     pdl_wait();
     pdl_launch_dependents();
@@ -275,7 +274,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_gn_backward(const __grid_consta
             }
         }
         const int64_t at = q.c - q.c0 + c;
-        if (q.rank == 0) a.part[q.n * a.t.C + at] = t;
+        if (q.rank == 0) {
+            if (a.N > 1) {
+                a.part[q.n * a.t.C + at] = t;
+            } else {  // nothing to add up
+                if (a.dbeta) a.dbeta[at] = t.x;
+                if (a.dgamma) a.dgamma[at] = t.y;
+            }
+        }
         const float gamma = a.gamma ? a.gamma[at] : 1.f;
         sh_all[c] = make_float2(gamma * t.x, gamma * t.y);
     }
@@ -330,26 +336,22 @@ cudaError_t launch_group_norm_backward(const GroupNorm& p, int sm_count, cudaStr
     const int channel_ctas = p.dgamma || p.dbeta ? (int)((p.C + 7) / 8) : 0;
     GnSlab slab;
     if (vec && a.t.ctas > 0) {
-        const int most = size == 4 ? 4 : 8;  // vectors a thread can hold
-        int u = 0;
-        if (gn_slab(p.N, p.P, p.C, p.G, (int)size, false, 2, slab) && slab.ctas <= (int64_t)sm_count * kGnFewCtas) u = 2;
-        else if (getenv("GN_MOST") && gn_slab(p.N, p.P, p.C, p.G, (int)size, false, most, slab)) u = most;
+        const int u = gn_vectors(p.N, p.P, p.C, p.G, (int)size, false, 4, kGnBackwardWork, sm_count, slab);
         if (u) {
             launch_begin("k_gn_backward", stream);
             cudaError_t e = with_dtype(p.dtype, [&](auto elem) {
                 using E = decltype(elem);
-                constexpr int M = sizeof(E) == 4 ? 4 : 8;
                 return with_act(p.act, [&](auto act) {
                     constexpr int A = decltype(act)::value;
                     return with_bool(kept, [&](auto k) {
                         constexpr bool K = decltype(k)::value;
                         return u == 2 ? launch_cluster(k_gn_backward<E, A, K, 2>, slab.ctas, slab.cluster, stream, a, slab)
-                                      : launch_cluster(k_gn_backward<E, A, K, M>, slab.ctas, slab.cluster, stream, a, slab);
+                                      : launch_cluster(k_gn_backward<E, A, K, 4>, slab.ctas, slab.cluster, stream, a, slab);
                     });
                 });
             });
             launch_end(stream);
-            if (e != cudaSuccess || channel_ctas == 0) return e;
+            if (e != cudaSuccess || channel_ctas == 0 || p.N == 1) return e;
             a.t.chunks = 1;  // a pair of sums per sample and channel
             launch_begin("k_gn_grad_join", stream);
             e = launch_pdl(k_gn_grad_join, channel_ctas, kThreads, 0, stream, a, 0);
@@ -361,7 +363,7 @@ cudaError_t launch_group_norm_backward(const GroupNorm& p, int sm_count, cudaStr
     const auto launch = [&](auto which) {
         constexpr bool kSums = decltype(which)::value;
         const auto one = [&](auto kernel, int V) {
-            a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, V, gn_wave(kernel, sm_count), kSums ? kGnMinPx : kGnMinPxApply));
+            a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, V, gn_wave(kernel, sm_count), kSums ? kGnMinChunk : 2));
             if (a.t.ctas == 0) return cudaSuccess;
             launch_begin(kSums ? "k_gn_grad_sums" : "k_gn_grad", stream);
             const cudaError_t r = launch_pdl(kernel, (int)a.t.ctas, kThreads, 0, stream, a);

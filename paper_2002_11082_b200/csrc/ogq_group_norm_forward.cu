@@ -4,7 +4,6 @@
 //   Moments are sums about the first value a thread sees: that value is one of those summed, so the sum of squares about the
 // mean is at least (1 - 1/n) of its squared distance d to the mean, while what is subtracted is n d^2: with n <= 64 pixels a thread the
 // difference loses at most a factor 64 of fp32's 2^-24.  Joining two sets adds n_a n_b / (n_a + n_b) (mean_a - mean_b)^2, all positive.
-#include <stdlib.h>
 #include "ogq_group_norm_resident.cuh"
 
 namespace ogq {
@@ -169,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) k_gn_apply(const __grid_constant__ G
 // The whole pass of one slab (see ogq_group_norm_resident.cuh): x is read once.  The CTA's mean and its sum of squares about that
 // mean, then joined over the cluster.
 template <class E, int ACT, int KEEP, int U>
-__global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : 3) k_gn_forward(const __grid_constant__ GnArgs a, const __grid_constant__ GnSlab s)
+__global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_forward(const __grid_constant__ GnArgs a, const __grid_constant__ GnSlab s)
 {
     pdl_wait();
     pdl_launch_dependents();
@@ -327,26 +326,25 @@ cudaError_t launch_group_norm_forward(const GroupNorm& p, int sm_count, cudaStre
     const bool vec = p.C % 8 == 0 && gn_aligned(p.x, 16) && gn_aligned(p.out, 16) && (p.C * size) % 16 == 0;
     const bool fused = p.codes && vec && p.C % kAct8Group == 0 && gn_aligned(p.codes, 8);
     GnSlab slab;
-    const int most = size == 4 ? 4 : 8;  // vectors a thread can hold
     if (vec && p.P > 0 && (!p.codes || fused)) {
-        // few CTAs: two vectors a thread, which makes more of them and each quicker
-        int u = 0;
-        if (gn_slab(p.N, p.P, p.C, p.G, (int)size, fused, 2, slab) && slab.ctas <= (int64_t)sm_count * kGnFewCtas) u = 2;
-        else if (getenv("GN_MOST") && gn_slab(p.N, p.P, p.C, p.G, (int)size, fused, most, slab)) u = most;
+        const int u = gn_vectors(p.N, p.P, p.C, p.G, (int)size, fused, size == 4 ? 4 : 8, kGnForwardWork, sm_count, slab);
         if (u) {
             const GnArgs a = gn_args(p, gn_tiles(p.N, p.P, p.C, p.G, 8, sm_count, 1));
             launch_begin("k_gn_forward", stream);
             const cudaError_t e = with_dtype(p.dtype, [&](auto elem) {
                 using E = decltype(elem);
-                constexpr int M = sizeof(E) == 4 ? 4 : 8;
                 return with_act(p.act, [&](auto act) {
                     constexpr int A = decltype(act)::value;
-                    return with_bool(u == 2, [&](auto few) {
-                        constexpr int U = decltype(few)::value ? 2 : M;
+                    const auto with = [&](auto vectors) {
+                        constexpr int U = decltype(vectors)::value;
                         if (!fused) return launch_cluster(k_gn_forward<E, A, 0, U>, slab.ctas, slab.cluster, stream, a, slab);
                         if (p.rounding == OGQ_ROUND_RANDOM) return launch_cluster(k_gn_forward<E, A, 2, U>, slab.ctas, slab.cluster, stream, a, slab);
                         return launch_cluster(k_gn_forward<E, A, 1, U>, slab.ctas, slab.cluster, stream, a, slab);
-                    });
+                    };
+                    if constexpr (sizeof(E) == 2) {
+                        if (u == 8) return with(std::integral_constant<int, 8>{});
+                    }
+                    return u == 4 ? with(std::integral_constant<int, 4>{}) : with(std::integral_constant<int, 2>{});
                 });
             });
             launch_end(stream);
@@ -374,7 +372,7 @@ cudaError_t launch_group_norm_forward(const GroupNorm& p, int sm_count, cudaStre
     GnArgs sums;
     e = with_dtype(p.dtype, [&](auto elem) {
         using E = decltype(elem);
-        return vec ? launch("k_gn_moments", k_gn_moments<E, 8>, 8, kGnMinPx, sums) : launch("k_gn_moments", k_gn_moments<E, 1>, 1, kGnMinPx, sums);
+        return vec ? launch("k_gn_moments", k_gn_moments<E, 8>, 8, kGnMinChunk, sums) : launch("k_gn_moments", k_gn_moments<E, 1>, 1, kGnMinChunk, sums);
     });
     if (e != cudaSuccess) return e;
     launch_begin("k_gn_stats", stream);
@@ -384,12 +382,12 @@ cudaError_t launch_group_norm_forward(const GroupNorm& p, int sm_count, cudaStre
     return with_dtype(p.dtype, [&](auto elem) {
         using E = decltype(elem);
         GnArgs a;
-        if (!vec) return launch("k_gn_apply", k_gn_apply<E, 1, -1, 0>, 1, kGnMinPxApply, a);
+        if (!vec) return launch("k_gn_apply", k_gn_apply<E, 1, -1, 0>, 1, 2, a);
         return with_act(p.act, [&](auto act) {
             constexpr int A = decltype(act)::value;
-            if (!fused) return launch("k_gn_apply", k_gn_apply<E, 8, A, 0>, 8, kGnMinPxApply, a);
-            if (p.rounding == OGQ_ROUND_RANDOM) return launch("k_gn_apply", k_gn_apply<E, 8, A, 2>, 8, kGnMinPxApply, a);
-            return launch("k_gn_apply", k_gn_apply<E, 8, A, 1>, 8, kGnMinPxApply, a);
+            if (!fused) return launch("k_gn_apply", k_gn_apply<E, 8, A, 0>, 8, 2, a);
+            if (p.rounding == OGQ_ROUND_RANDOM) return launch("k_gn_apply", k_gn_apply<E, 8, A, 2>, 8, 2, a);
+            return launch("k_gn_apply", k_gn_apply<E, 8, A, 1>, 8, 2, a);
         });
     });
 }

@@ -9,7 +9,10 @@ namespace ogq {
 
 constexpr int kGnMaxCluster = 8;    // the portable size
 constexpr int kGnMaxWidth = 512;    // channels of a slab
-constexpr int kGnFewCtas = 4;       // per SM: up to these, two vectors a thread
+// Vectors per thread of an SM's CTAs, up to which a slab's pass is faster than streaming (32 x 3136 x 64 bf16: forward, 24 a thread and
+// SM, 19 us against 23; backward, 28, 34 us against 24).
+constexpr int kGnForwardWork = 32, kGnBackwardWork = 16;
+constexpr int kGnMostCtas = 8;      // per SM: with more of them a thread takes more vectors (32 x 196 x 1024 bf16 forward: 24 us with two each, 15 with four)
 
 struct GnSlab {
     int width;      // channels of a slab
@@ -24,16 +27,16 @@ struct GnSlab {
     int64_t ctas;
 };
 
-// The slab of the smallest width that is whole groups, whole vectors, whole units of 32 where x is kept, and at least 64 bytes;
+// The slab of the smallest width that is whole groups, whole vectors, whole units of 32 where x is kept, and at least `bytes` wide;
 // false where none divides C or P pixels do not fit U to a thread.
-inline bool gn_slab(int64_t N, int64_t P, int64_t C, int64_t G, int size, bool keep, int U, GnSlab& s)
+inline bool gn_slab(int64_t N, int64_t P, int64_t C, int64_t G, int size, bool keep, int U, int bytes, GnSlab& s)
 {
     const int64_t per = C / G, unit = keep ? 32 : 8;
     int64_t least = unit;
     while (least % per != 0 && least <= kGnMaxWidth) least += unit;
     int64_t width = 0;
     for (int64_t w = least; w <= kGnMaxWidth && w <= C; w += least)
-        if (C % w == 0 && (w * size >= 64 || w == C)) { width = w; break; }
+        if (C % w == 0 && (w * size >= bytes || w == C)) { width = w; break; }
     if (width == 0) return false;
     s.width = (int)width;
     s.wv = (int)(width / 8);
@@ -49,6 +52,18 @@ inline bool gn_slab(int64_t N, int64_t P, int64_t C, int64_t G, int size, bool k
     s.sum_rows = s.in_warp ? kWarps : s.rows;
     s.ctas = N * s.slabs * k;
     return s.ctas <= 0x7fffffff;
+}
+
+// The fewest vectors a thread, of 2, 4 and (most = 8) 8, for which the slabs fit and are little enough work; 0: none.  Slabs of whole pairs of
+// sectors, or single ones (whose other half another CTA asks for at the same time) where those hold too few pixels.
+inline int gn_vectors(int64_t N, int64_t P, int64_t C, int64_t G, int size, bool keep, int most, int work, int sm_count, GnSlab& s)
+{
+    for (int bytes = 64; bytes >= 32; bytes /= 2)
+        for (int u = 2; u <= most; u *= 2)
+            if (gn_slab(N, P, C, G, size, keep, u, bytes, s) && s.ctas <= (int64_t)sm_count * kGnMostCtas &&
+                s.ctas * u <= (int64_t)sm_count * work)
+                return u;
+    return 0;
 }
 
 __device__ __forceinline__ uint32_t gn_rank()
