@@ -27,7 +27,7 @@ constexpr int kOperands = 2;                   // converted tiles of x^: one bei
 constexpr int kTileM = 256;                    // columns of dy per tile (both CTAs)
 constexpr int kABytes = 128 * kStepRows * 2;   // dy's tile of one CTA
 constexpr int kScaleBytes = kStepRows * 16;    // scales around those of a tile's (at most four) groups: 16 bytes a row by TMA, or two words
-constexpr int kWgThreads = 640;                // a warpgroup for TMA, MMA, TMEM and units; two of converters; two that take sums out of TMEM
+constexpr int kWgThreads = 640;                // a warpgroup for TMA, MMA, TMEM, scales and bias; two of converters; two that take sums out of TMEM
 // Registers a thread of the three kinds; the block starts with 640 * 96 = 61,440, which the split must not exceed.
 constexpr int kRegsStart = 96, kRegsControl = 48, kRegsConvert = 64, kRegsSums = 152;
 static_assert(128 * kRegsControl + 256 * kRegsConvert + 256 * kRegsSums <= kWgThreads * kRegsStart, "a warpgroup would wait for registers for ever");
@@ -48,6 +48,8 @@ template <int BN> struct WgShape {
     static constexpr int kSlotFloats = 128 * BN;                  // a partial tile of one CTA
 };
 
+__host__ __device__ inline int64_t bias_pitch(int64_t out_cols) { return (out_cols + 3) / 4 * 4; }
+
 struct WgArgs {
     const uint8_t* scales;
     float* dw;
@@ -65,6 +67,12 @@ struct WgArgs {
     bool accumulate;
     bool wide;          // 32-byte stores
     bool tma_scales;    // a multiple of 16 groups: TMA copies the scales
+    // Bias (db not null): from partial sums over `chunks` parts of the rows, or (chunks = 0, one step) from dy.
+    float* db;
+    const float* bias_parts;  // [chunks][bias_pitch]
+    int chunks;
+    const uint16_t* dy;       // as TMA reads it: bf16, dy_rows rows of stride ld_dy
+    int64_t ld_dy, dy_rows;
 };
 
 // The pieces of work of one pair: (tile, steps [k0, k1)), the same sequence in every role.
@@ -170,6 +178,44 @@ __device__ __forceinline__ void wg_store8(const WgArgs& a, int64_t o, int64_t i,
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (i + j < a.cols) w[j] = a.accumulate ? w[j] + v[j] : v[j];
+}
+
+// db of four columns from o on, a multiple of 4.
+__device__ __forceinline__ void wg_bias(const WgArgs& a, int64_t o)
+{
+    if (o >= a.out_cols) return;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (a.chunks > 0) {
+#pragma unroll 4
+        for (int k = 0; k < a.chunks; ++k) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(a.bias_parts + k * bias_pitch(a.out_cols) + o));
+            sum[0] = __fadd_rn(sum[0], v.x);
+            sum[1] = __fadd_rn(sum[1], v.y);
+            sum[2] = __fadd_rn(sum[2], v.z);
+            sum[3] = __fadd_rn(sum[3], v.w);
+        }
+    } else {
+        const uint16_t* p = a.dy + o;
+        const bool four = o + 3 < a.out_cols;
+#pragma unroll 8
+        for (int t = 0; t < (int)a.dy_rows; ++t) {
+            uint2 v = make_uint2(0u, 0u);
+            if (four) {
+                v = *reinterpret_cast<const uint2*>(p + t * a.ld_dy);
+            } else {
+                v.x = p[t * a.ld_dy];
+                if (o + 1 < a.out_cols) v.x |= (uint32_t)p[t * a.ld_dy + 1] << 16;
+                if (o + 2 < a.out_cols) v.y = p[t * a.ld_dy + 2];
+            }
+            sum[0] = __fadd_rn(sum[0], __uint_as_float(v.x << 16));
+            sum[1] = __fadd_rn(sum[1], __uint_as_float(v.x & 0xffff0000u));
+            sum[2] = __fadd_rn(sum[2], __uint_as_float(v.y << 16));
+            sum[3] = __fadd_rn(sum[3], __uint_as_float(v.y & 0xffff0000u));
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (o + j < a.out_cols) a.db[o + j] = a.accumulate ? a.db[o + j] + sum[j] : sum[j];
 }
 
 template <int BN>
@@ -301,13 +347,22 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
                 }
             }
         }
-        else if (warp == 3 && !a.tma_scales) {  // scales: the aligned words around each row's bytes, never past the end
+        else if (warp == 3) {
+            if (a.db) {  // bias: of each column of tiles, by the CTAs that begin its first tile
+                WgWork w(a, pair);
+                while (w.next(a, pair)) {
+                    int m, n;
+                    wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
+                    if (n == 0 && w.k0 == 0) wg_bias(a, (int64_t)m * kTileM + rank * 128 + lane * 4);
+                }
+            }
+            // scales that TMA does not copy: the aligned words around each row's bytes, never past the end
             WgWork w(a, pair);
             int s = 0;
             uint32_t phase = 1;
             bool ok = true;
             const int64_t all = a.rows * a.groups;
-            while (ok && w.next(a, pair)) {
+            while (!a.tma_scales && ok && w.next(a, pair)) {
                 int m, n;
                 wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
                 const int first = (n * BN + (int)rank * S::kCols) / kAct8Group;
@@ -545,12 +600,27 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_bias(const __grid_constant__
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = 0.f;
     if (c < a.out_cols) {
-        for (int64_t t = k * a.chunk + warp; t < end; t += kWarps) {
-            float v[V];
-            if constexpr (V == 8) unpack8(load_raw8((const E*)a.dy + t * a.ld_dy + c), v);
-            else v[0] = load1((const E*)a.dy + t * a.ld_dy + c);
+        constexpr int kAtOnce = 8;
+        const E* p = (const E*)a.dy + c;
+        for (int64_t t = k * a.chunk + warp; t < end; t += kAtOnce * kWarps) {
+            if constexpr (V == 8) {
+                Raw8<E> r[kAtOnce];
 #pragma unroll
-            for (int j = 0; j < V; ++j) s[j] = __fadd_rn(s[j], v[j]);
+                for (int u = 0; u < kAtOnce; ++u) r[u] = t + u * kWarps < end ? load_raw8(p + (t + u * kWarps) * a.ld_dy) : zero_raw8<E>();
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) {
+                    float v[V];
+                    unpack8(r[u], v);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) s[j] = __fadd_rn(s[j], v[j]);
+                }
+            } else {
+                float v[kAtOnce];
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) v[u] = t + u * kWarps < end ? load1(p + (t + u * kWarps) * a.ld_dy) : 0.f;
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) s[0] = __fadd_rn(s[0], v[u]);
+            }
         }
     }
 #pragma unroll
@@ -563,7 +633,7 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_bias(const __grid_constant__
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) sum += sh[w][i];
         if (a.chunks == 1) a.db[o] = a.accumulate ? a.db[o] + sum : sum;
-        else a.part[k * a.out_cols + o] = sum;
+        else a.part[k * bias_pitch(a.out_cols) + o] = sum;
     }
 }
 
@@ -574,7 +644,7 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_bias_join(const __grid_const
     const int64_t o = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (o >= a.out_cols) return;
     double s = 0.0;
-    for (int k = 0; k < a.chunks; ++k) s += (double)__ldcg(a.part + (int64_t)k * a.out_cols + o);
+    for (int k = 0; k < a.chunks; ++k) s += (double)__ldcg(a.part + k * bias_pitch(a.out_cols) + o);
     a.db[o] = a.accumulate ? (float)((double)a.db[o] + s) : (float)s;
 }
 
@@ -597,6 +667,7 @@ namespace {
 
 constexpr int64_t kLayoutBytes = (int64_t)40 << 20;  // of operands laid out at a time: they stay in L2 until they are read
 constexpr int kBiasCtas = 4;                         // per SM
+constexpr int64_t kBiasRows = 64;                    // up to these, no kernel of its own
 
 int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 int terms_of(int dtype) { return dtype == OGQ_F32 ? 3 : dtype == OGQ_F16 ? 2 : 1; }
@@ -641,7 +712,7 @@ Plan make_plan(int64_t rows, int64_t cols, int64_t out_cols, int dtype, bool lay
     if (p.bias_chunk < 1) p.bias_chunk = 1;
     p.bias_chunks = (int)((rows + p.bias_chunk - 1) / p.bias_chunk);
     if (p.bias_chunks < 1) p.bias_chunks = 1;
-    p.bias_bytes = up_to((int64_t)p.bias_chunks * out_cols * 4, 256);
+    p.bias_bytes = up_to(p.bias_chunks * bias_pitch(out_cols) * 4, 256);
     return p;
 }
 
@@ -685,6 +756,12 @@ cudaError_t launch_product(const CUtensorMap& map_dy, const CUtensorMap& map_x, 
     if (a.per < kMinSteps) a.per = a.steps < kMinSteps ? a.steps : kMinSteps;
     if (left == 0) a.per = a.steps;
     const int64_t busy = a.whole ? a.pairs : (a.rest + a.per - 1) / a.per;
+    // A build whose kernel starts with fewer registers than the split needs would wait for them for ever: it is not launched.
+    static const bool starts_with_all = [] {
+        cudaFuncAttributes f;
+        return cudaFuncGetAttributes(&f, k_wgrad<BN>) == cudaSuccess && f.numRegs >= kRegsStart;
+    }();
+    if (!starts_with_all) return cudaErrorInvalidConfiguration;
     cudaError_t e = cudaFuncSetAttribute(k_wgrad<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, WgShape<BN>::kSmem);
     if (e != cudaSuccess) return e;
     launch_begin("k_wgrad", stream);
@@ -750,7 +827,13 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
     int8_t* kept = (int8_t*)((char*)terms + plan.terms_bytes);
     uint8_t* scales_to = (uint8_t*)kept + plan.kept_bytes;
 
-    if (p.db) {
+    // One step of bf16 rows: the product's kernel adds up dy for the bias as well.  More: a kernel before it leaves sums over chunks of
+    // rows, which the product's kernel joins.  (All of it there, by the warp that TMA leaves free, took the product from 430 to 610 us at
+    // 16,384 x 4096 x 4096, against 30 us for the other kernel.)
+    const bool narrow = p.cols <= 128;
+    const bool tma_scales = act8_groups(p.cols) % 16 == 0 && (lay_s || ((uintptr_t)p.scales & 15) == 0);
+    const bool beside = p.db && p.cols > 0 && p.rows <= kBiasRows && p.dtype == OGQ_BF16;
+    if (p.db && !beside) {
         const int size = p.dtype == OGQ_F32 ? 4 : 2;
         const bool vec = ((uintptr_t)p.dy & 15) == 0 && p.ld_dy * size % 16 == 0 && p.ld_dy % 8 == 0 && p.out_cols % 8 == 0;
         WgBias b = {p.dy, p.ld_dy, p.rows, p.out_cols, plan.bias_chunk, bias_part, p.db, plan.bias_chunks, 0, acc};
@@ -762,7 +845,7 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
                        : launch_pdl(k_wgrad_bias<E, 1>, b.ctiles * b.chunks, kThreads, 0, stream, b);
         });
         launch_end(stream);
-        if (e == cudaSuccess && b.chunks > 1) {
+        if (e == cudaSuccess && b.chunks > 1 && p.cols == 0) {
             launch_begin("k_wgrad_bias_join", stream);
             e = launch_pdl(k_wgrad_bias_join, (int)((p.out_cols + kThreads - 1) / kThreads), kThreads, 0, stream, b);
             launch_end(stream);
@@ -799,7 +882,6 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
             if (e != cudaSuccess) return e;
         }
         CUtensorMap map_dy, map_x, map_scales;
-        const bool narrow = p.cols <= 128;
         const int terms_here = lay_dy ? plan.terms : 1;
         if (!make_map(&map_dy, lay_dy ? (const void*)terms : dy, true, p.out_cols, lay_dy ? terms_here * padded : rows,
                       (lay_dy ? plan.ld_terms : p.ld_dy) * 2, 64) ||
@@ -808,13 +890,22 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
         // Scales a row apart are 64 requests a step either way, but copied by a warp they also take 128 cycles a step from the shared
         // memory pipe, which is what bounds the loop (16,384 x 4096 x 4096: 504 -> 404 us with TMA).
         a.scales = lay_s ? scales_to : scales;
-        a.tma_scales = a.groups % 16 == 0 && ((uintptr_t)a.scales & 15) == 0;
+        a.tma_scales = tma_scales;
         if (!a.tma_scales) map_scales = map_x;  // not used
         else if (!make_map(&map_scales, a.scales, false, a.groups, rows, a.groups, 16)) return cudaErrorInvalidValue;
         a.rows = rows;
         a.steps_x = (int)(padded / kStepRows);
         a.steps = terms_here * a.steps_x;
         a.accumulate = acc || t > 0;
+        a.db = nullptr;
+        if (t == 0 && (beside || (p.db && plan.bias_chunks > 1))) {
+            a.db = p.db;
+            a.bias_parts = bias_part;
+            a.chunks = beside ? 0 : plan.bias_chunks;
+            a.dy = lay_dy ? terms : (const uint16_t*)dy;
+            a.ld_dy = lay_dy ? plan.ld_terms : p.ld_dy;
+            a.dy_rows = rows;
+        }
         e = narrow ? launch_product<128>(map_dy, map_x, map_scales, a, stream) : launch_product<256>(map_dy, map_x, map_scales, a, stream);
         if (e != cudaSuccess) return e;
     }

@@ -130,3 +130,20 @@ def test_long_sums_and_the_same_bits_again(rows, cols, out, dtype):
     for _ in range(3):
         dw2, db2 = run(dy, out, codes, scales, rows, cols, out, d)
         assert torch.equal(dw.t, dw2.t) and torch.equal(db.t, db2.t)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,cols,out", [(32, 2048, 300), (128, 130, 70), (129, 2049, 258), (700, 2304, 513), (2000, 4096, 1000), (1, 2048, 1)])
+def test_bias_beside_the_product(dtype, rows, cols, out):
+    """Eight tiles of a column and more, or one step of 128 rows: the product's kernel adds up dy itself; added to what is there too."""
+    d, dt = DTYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(rows + cols)
+    codes, scales = kept_matrix(gen, rows, cols)
+    ld = (out + 7) // 8 * 8
+    dy = Guarded(rows, out, ld, dt, 0, torch.randn(rows, out, device="cuda", generator=gen).to(dt))
+    x = decoded(codes, scales)
+    dw, db = run(dy.t, ld, codes, scales, rows, cols, out, d)
+    check(dy.t, x, dw, db)
+    w0, b0 = dw.t.clone(), db.t.clone()
+    run(dy.t, ld, codes, scales, rows, cols, out, d, 1, dw, db)
+    check(dy.t, x, dw, db, w0.double(), b0[0].double())
