@@ -29,7 +29,7 @@ constexpr int kABytes = 128 * kStepRows * 2;   // dy's tile of one CTA
 constexpr int kScaleBytes = kStepRows * 16;    // scales around those of a tile's (at most four) groups: 16 bytes a row by TMA, or two words
 constexpr int kWgThreads = 640;                // a warpgroup for TMA, MMA, TMEM, scales and bias; two of converters; two that take sums out of TMEM
 // Registers a thread of the three kinds; the block starts with 640 * 96 = 61,440, which the split must not exceed.
-constexpr int kRegsStart = 96, kRegsControl = 48, kRegsConvert = 64, kRegsSums = 152;
+constexpr int kRegsStart = 96, kRegsControl = 64, kRegsConvert = 56, kRegsSums = 152;
 static_assert(128 * kRegsControl + 256 * kRegsConvert + 256 * kRegsSums <= kWgThreads * kRegsStart, "a warpgroup would wait for registers for ever");
 constexpr uint32_t kTmemColumns = 512;
 constexpr int kMinSteps = 4;                   // fewer steps than these are not split: a second launch costs more than they do
@@ -60,6 +60,7 @@ struct WgArgs {
     int tiles_m, tiles_n;
     int steps;          // of a tile: terms * steps_x
     int steps_x;        // steps over x^'s rows
+    int last_rows;      // of the last of them that are multiplied, a multiple of 16 (dy's tile is zero below, x^ is not converted)
     int pairs;
     int whole;          // tiles per pair that are done alone
     int64_t rest;       // steps of the tiles left
@@ -129,30 +130,42 @@ __device__ __forceinline__ uint32_t wg_value2(uint32_t p, __nv_bfloat162 unit)
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// This thread's rows, eight codes each, of the stage's codes, scales (from this thread's byte on) and place for the operand.  Eight lanes write the 128
-// bytes of a row of a swizzled block: no bank conflicts.
-template <int BN>
-__device__ __forceinline__ void wg_convert(uint32_t raw, uint32_t scales, int pitch, uint32_t b, int row, int oct)
+// Eight codes of row t and their scale byte into the row's place in the operand.
+__device__ __forceinline__ void wg_put8(uint32_t x, uint32_t y, uint32_t byte, uint32_t b, int t, int oct)
 {
-    constexpr int kCols = WgShape<BN>::kCols, kEach = WgShape<BN>::kRowsEach;
+    const uint32_t both = byte * 0x800080u;  // the byte is a bf16 number's exponent
+    const __nv_bfloat162 unit = *reinterpret_cast<const __nv_bfloat162*>(&both);
+    const uint32_t v0 = wg_value2(__byte_perm(x, 0, 0x4140), unit), v1 = wg_value2(__byte_perm(x, 0, 0x4342), unit);
+    const uint32_t v2 = wg_value2(__byte_perm(y, 0, 0x4140), unit), v3 = wg_value2(__byte_perm(y, 0, 0x4342), unit);
+    const uint32_t at = b + (oct >> 3) * (kStepRows * 128) + t * 128 + (((oct ^ t) & 7) << 4);
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(at), "r"(v0), "r"(v1), "r"(v2), "r"(v3) : "memory");
+}
+
+// This thread's rows below `rows`, eight codes each, of the stage's codes, scales (from this thread's byte on) and place for the
+// operand.  Eight lanes write the 128 bytes of a row of a swizzled block: no bank conflicts.
+template <int BN>
+__device__ __forceinline__ void wg_convert(uint32_t raw, uint32_t scales, int pitch, uint32_t b, int row, int oct, int rows)
+{
+    constexpr int kCols = WgShape<BN>::kCols, kEach = WgShape<BN>::kRowsEach, kStep = WgShape<BN>::kRowsAtOnce;
+    if (rows < kStepRows) {  // the last step
+#pragma unroll 1
+        for (int t = row; t < rows && t < row + kEach * kStep; t += kStep) {
+            uint32_t x, y, u;
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(raw + t * kCols + oct * 8));
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(u) : "r"(scales + t * pitch));
+            wg_put8(x, y, u, b, t, oct);
+        }
+        return;
+    }
     uint32_t c[kEach][2], u[kEach];  // all loads before the first store, which none could pass
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        const int t = row + WgShape<BN>::kRowsAtOnce * j;
+        const int t = row + kStep * j;
         asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(c[j][0]), "=r"(c[j][1]) : "r"(raw + t * kCols + oct * 8));
         asm volatile("ld.shared.u8 %0, [%1];" : "=r"(u[j]) : "r"(scales + t * pitch));
     }
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        const int t = row + WgShape<BN>::kRowsAtOnce * j;
-        const uint32_t x = c[j][0], y = c[j][1];
-        const uint32_t both = u[j] * 0x800080u;  // the byte is a bf16 number's exponent
-        const __nv_bfloat162 unit = *reinterpret_cast<const __nv_bfloat162*>(&both);
-        const uint32_t v0 = wg_value2(__byte_perm(x, 0, 0x4140), unit), v1 = wg_value2(__byte_perm(x, 0, 0x4342), unit);
-        const uint32_t v2 = wg_value2(__byte_perm(y, 0, 0x4140), unit), v3 = wg_value2(__byte_perm(y, 0, 0x4342), unit);
-        const uint32_t at = b + (oct >> 3) * (kStepRows * 128) + t * 128 + (((oct ^ t) & 7) << 4);
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(at), "r"(v0), "r"(v1), "r"(v2), "r"(v3) : "memory");
-    }
+    for (int j = 0; j < kEach; ++j) wg_put8(c[j][0], c[j][1], u[j], b, row + kStep * j, oct);
 }
 
 __device__ __forceinline__ void store8_wide(float* p, const float* v)
@@ -180,6 +193,27 @@ __device__ __forceinline__ void wg_store8(const WgArgs& a, int64_t o, int64_t i,
         if (i + j < a.cols) w[j] = a.accumulate ? w[j] + v[j] : v[j];
 }
 
+// Four lanes with four eights of values each: lane j's eight r becomes lane r's eight j.
+__device__ __forceinline__ void wg_exchange(float* v, int lane)
+{
+#pragma unroll
+    for (int bit = 1; bit <= 2; bit *= 2) {
+        const bool high = lane & bit;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (r & bit) continue;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float& a = v[r * 8 + j];
+                float& b = v[(r | bit) * 8 + j];
+                const float got = __shfl_xor_sync(0xffffffffu, high ? a : b, bit);
+                if (high) a = got;
+                else b = got;
+            }
+        }
+    }
+}
+
 // db of four columns from o on, a multiple of 4.
 __device__ __forceinline__ void wg_bias(const WgArgs& a, int64_t o)
 {
@@ -196,21 +230,33 @@ __device__ __forceinline__ void wg_bias(const WgArgs& a, int64_t o)
         }
     } else {
         const uint16_t* p = a.dy + o;
-        const bool four = o + 3 < a.out_cols;
-#pragma unroll 8
-        for (int t = 0; t < (int)a.dy_rows; ++t) {
-            uint2 v = make_uint2(0u, 0u);
-            if (four) {
-                v = *reinterpret_cast<const uint2*>(p + t * a.ld_dy);
+        const int rows = (int)a.dy_rows;
+        constexpr int kAtOnce = 8;
+        for (int t = 0; t < rows; t += kAtOnce) {
+            uint2 v[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) v[k] = make_uint2(0u, 0u);
+            if (o + 3 < a.out_cols) {
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k)
+                    if (t + k < rows) v[k] = *reinterpret_cast<const uint2*>(p + (t + k) * a.ld_dy);
             } else {
-                v.x = p[t * a.ld_dy];
-                if (o + 1 < a.out_cols) v.x |= (uint32_t)p[t * a.ld_dy + 1] << 16;
-                if (o + 2 < a.out_cols) v.y = p[t * a.ld_dy + 2];
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    if (t + k >= rows) break;
+                    const uint16_t* q = p + (t + k) * a.ld_dy;
+                    v[k].x = q[0];
+                    if (o + 1 < a.out_cols) v[k].x |= (uint32_t)q[1] << 16;
+                    if (o + 2 < a.out_cols) v[k].y = q[2];
+                }
             }
-            sum[0] = __fadd_rn(sum[0], __uint_as_float(v.x << 16));
-            sum[1] = __fadd_rn(sum[1], __uint_as_float(v.x & 0xffff0000u));
-            sum[2] = __fadd_rn(sum[2], __uint_as_float(v.y << 16));
-            sum[3] = __fadd_rn(sum[3], __uint_as_float(v.y & 0xffff0000u));
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                sum[0] = __fadd_rn(sum[0], __uint_as_float(v[k].x << 16));
+                sum[1] = __fadd_rn(sum[1], __uint_as_float(v[k].x & 0xffff0000u));
+                sum[2] = __fadd_rn(sum[2], __uint_as_float(v[k].y << 16));
+                sum[3] = __fadd_rn(sum[3], __uint_as_float(v[k].y & 0xffff0000u));
+            }
         }
     }
 #pragma unroll
@@ -326,6 +372,7 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
             bool ok = true;
             constexpr uint32_t instruction = instruction_bf16(kTileM, BN);
             while (ok && w.next(a, pair)) {
+                int x = w.k0 % a.steps_x;
                 for (int k = w.k0; ok && k < w.k1; k += kFlush) {
                     const int last = k + kFlush < w.k1 ? k + kFlush : w.k1;
                     if (!(ok = mbar_wait(taken(d), dphase, &failed))) break;
@@ -334,9 +381,15 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
                         if (!(ok = mbar_wait(dy_here(s), phase, &failed) && mbar_wait(op_here(b), bphase, &failed))) break;
                         tcgen05_fence_after();
                         const uint64_t da = tile_descriptor(stage_a(s), kStepRows * 128), db = tile_descriptor(operand_b(b), kStepRows * 128);
+                        if (++x < a.steps_x) {
 #pragma unroll
-                        for (int j = 0; j < kStepRows / 16; ++j)  // 16 rows are 2048 bytes on
-                            mma_bf16_pair(tmem + d * BN, da + j * (2048 >> 4), db + j * (2048 >> 4), instruction, q > k || j > 0);
+                            for (int j = 0; j < kStepRows / 16; ++j)  // 16 rows are 2048 bytes on
+                                mma_bf16_pair(tmem + d * BN, da + j * (2048 >> 4), db + j * (2048 >> 4), instruction, q > k || j > 0);
+                        } else {
+                            x = 0;
+                            for (int j = 0; j < a.last_rows / 16; ++j)
+                                mma_bf16_pair(tmem + d * BN, da + j * (2048 >> 4), db + j * (2048 >> 4), instruction, q > k || j > 0);
+                        }
                         mma_commit_pair(done(s));
                         if (++b == kOperands) { b = 0; bphase ^= 1; }
                         if (++s == kStages) { s = 0; phase ^= 1; }
@@ -398,9 +451,11 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
             // this thread's byte of a row's; of words, the first holds the row's at a place that is the same eight rows on
             const int first = (n * BN + (int)rank * S::kCols) / kAct8Group;
             const int byte = (a.tma_scales ? first & 15 : (row * a.groups + first) & 3) + oct / 4;
+            int x = w.k0 % a.steps_x;
             for (int k = w.k0; k < w.k1; ++k) {
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(raw_here(s), phase, &failed) && mbar_wait(done(before), before_phase, &failed)))) break;
-                wg_convert<BN>(stage_raw(s), stage_scales(s) + byte, a.tma_scales ? 16 : 8, operand_b(b), row, oct);
+                wg_convert<BN>(stage_raw(s), stage_scales(s) + byte, a.tma_scales ? 16 : 8, operand_b(b), row, oct, x + 1 == a.steps_x ? a.last_rows : kStepRows);
+                if (++x == a.steps_x) x = 0;
                 fence_async_shared();
                 __syncwarp();
                 if (lane == 0) {
@@ -448,13 +503,19 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
             wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
             const int row = quarter * 32 + lane;
             if (w.slot < 0) {
-                const int64_t o = (int64_t)m * kTileM + rank * 128 + row, i = (int64_t)n * BN + half * kHalf;
+                // Four lanes exchange their rows' eights of columns, so that they write 128 bytes of one row at a time (a row a lane, 32
+                // bytes at a time: 4.1 us for a tile).
+                const int64_t o = (int64_t)m * kTileM + rank * 128 + (row & ~3), i = (int64_t)n * BN + half * kHalf + (lane & 3) * 8;
 #pragma unroll
-                for (int c = 0; c < kHalf; c += 8) {
-                    float v[8];
+                for (int c = 0; c < kHalf; c += 32) {
+                    wg_exchange(acc + c, lane);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = acc[c + j];
-                    wg_store8(a, o, i + c, v);
+                    for (int r = 0; r < 4; ++r) {
+                        float v[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] = acc[c + r * 8 + j];
+                        wg_store8(a, o + r, i + c, v);
+                    }
                 }
             } else {
                 float* slot = a.slots + ((int64_t)(pair * 2 + w.slot) * 2 + rank) * S::kSlotFloats;
@@ -896,6 +957,7 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
         a.rows = rows;
         a.steps_x = (int)(padded / kStepRows);
         a.steps = terms_here * a.steps_x;
+        a.last_rows = (int)up_to(rows - (int64_t)(a.steps_x - 1) * kStepRows, 16);
         a.accumulate = acc || t > 0;
         a.db = nullptr;
         if (t == 0 && (beside || (p.db && plan.bias_chunks > 1))) {
