@@ -520,7 +520,8 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
             } else {
                 float* slot = a.slots + ((int64_t)(pair * 2 + w.slot) * 2 + rank) * S::kSlotFloats;
 #pragma unroll
-                for (int c = 0; c < kHalf; c += 8) store8_wide(slot + ((half * kHalf + c) / 8 * 128 + row) * 8, acc + c);
+                for (int c = 0; c < kHalf; c += 8)
+                    if ((int64_t)n * BN + half * kHalf + c < a.cols) store8_wide(slot + ((half * kHalf + c) / 8 * 128 + row) * 8, acc + c);
             }
         }
     }
@@ -546,15 +547,31 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_join(const __grid_constant__
     const int piece = (blockIdx.x - j * kPerTile) * kRows + r;
     const int rank = piece / (128 * (BN / 8)), in = piece - rank * (128 * (BN / 8));
     const int oct = in / 128, row = in - oct * 128;
-    const int64_t first = (int64_t)j * a.steps / a.per, last = ((int64_t)(j + 1) * a.steps - 1) / a.per;
+    int m, n;
+    wg_tile_place(a.whole * a.pairs + j, a.tiles_m, a.tiles_n, m, n);
+    const int64_t begin = (int64_t)j * a.steps, first = begin / a.per, last = (begin + a.steps - 1) / a.per;
     if (first == last) return;  // done by one pair
+    if ((int64_t)n * BN + oct * 8 >= a.cols) return;  // all of the CTA: its rows have the same eight columns
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int64_t p = first + part; p <= last; p += PARTS) {
-        const int slot = p * a.per / a.steps == j ? 0 : 1;
-        const float4* s = reinterpret_cast<const float4*>(a.slots + ((p * 2 + slot) * 2 + rank) * WgShape<BN>::kSlotFloats + (int64_t)in * 8);
-        const float4 x = __ldcg(s), y = __ldcg(s + 1);
-        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-        v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+    constexpr int kAtOnce = 4;
+    for (int64_t p0 = first + part; p0 <= last; p0 += PARTS * kAtOnce) {
+        float4 x[kAtOnce], y[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int64_t p = p0 + k * PARTS;
+            x[k] = y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (p <= last) {
+                const int slot = p * a.per < begin ? 1 : 0;  // a pair that begins before this tile has it second
+                const float4* s = reinterpret_cast<const float4*>(a.slots + ((p * 2 + slot) * 2 + rank) * WgShape<BN>::kSlotFloats + (int64_t)in * 8);
+                x[k] = __ldcg(s);
+                y[k] = __ldcg(s + 1);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            v[0] += x[k].x; v[1] += x[k].y; v[2] += x[k].z; v[3] += x[k].w;
+            v[4] += y[k].x; v[5] += y[k].y; v[6] += y[k].z; v[7] += y[k].w;
+        }
     }
     if constexpr (PARTS > 1) {
         sh[part][r][0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -568,8 +585,6 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_join(const __grid_constant__
             v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
         }
     }
-    int m, n;
-    wg_tile_place(a.whole * a.pairs + j, a.tiles_m, a.tiles_n, m, n);
     wg_store8(a, (int64_t)m * kTileM + rank * 128 + row, (int64_t)n * BN + oct * 8, v);
 }
 
