@@ -18,50 +18,67 @@ struct BwdArgs {
     int act;              // of the kernel of single elements
 };
 
-// Any sizes, strides and addresses: a warp per group, a lane per element, four groups under way.
+// Any sizes, strides and addresses: eight lanes a group, elements l, l + 8, l + 16, l + 24 of it for lane l, two groups a lane under way.
 template <class E, bool GATED>
 __global__ void __launch_bounds__(kThreads) k_act8_backward_any(const __grid_constant__ BwdArgs a)
 {
     pdl_wait();
     pdl_launch_dependents();
     constexpr bool kAccurate = sizeof(E) == 4;
-    constexpr int kUnits = 4;
-    const int lane = threadIdx.x & 31;
-    for (uint32_t g0 = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * kUnits; g0 < a.all_groups; g0 += gridDim.x * kWarps * kUnits) {
-        float v[kUnits], u[kUnits], d[kUnits];
+    constexpr int kUnits = 2;
+    constexpr uint32_t kTeams = kThreads / 8;
+    const int l = threadIdx.x & 7;
+    const uint32_t team = threadIdx.x >> 3;
+    for (uint32_t g0 = blockIdx.x * (kTeams * kUnits) + team; g0 < a.all_groups; g0 += gridDim.x * (kTeams * kUnits)) {
+        float v[kUnits][4], u[kUnits][4], d[kUnits][4], unit[kUnits], up_unit[kUnits];
         uint32_t row[kUnits];
         int64_t col[kUnits];
-        bool in[kUnits];
+        int n[kUnits];  // of this lane's four elements
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-            row[k] = act8_row(a, g0 + k);
-            col[k] = (int64_t)(g0 + k - row[k] * a.groups) * kAct8Group + lane;
-            in[k] = g0 + k < a.all_groups && col[k] < a.cols;
-            if (!in[k]) continue;
+            const uint32_t g = g0 + k * kTeams;
+            row[k] = act8_row(a, g);
+            col[k] = (int64_t)(g - row[k] * a.groups) * kAct8Group + l;
+            n[k] = g < a.all_groups ? (int)(a.cols - col[k] >= 25 ? 4 : a.cols > col[k] ? (a.cols - col[k] + 7) / 8 : 0) : 0;
             const int64_t at = (int64_t)row[k] * a.cols + col[k];
-            v[k] = (float)a.codes[at] * act8_unit(a.scales[g0 + k]);
-            if (GATED) u[k] = (float)a.up_codes[at] * act8_unit(a.up_scales[g0 + k]);
-            if (a.dy) d[k] = load1((const E*)a.dy + row[k] * a.ld_dy + col[k]);
+            if (n[k] > 0) {
+                unit[k] = act8_unit(a.scales[g]);
+                if (GATED) up_unit[k] = act8_unit(a.up_scales[g]);
+            }
+            const E* dy = (const E*)a.dy + row[k] * a.ld_dy + col[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (e >= n[k]) break;
+                v[k][e] = (float)a.codes[at + 8 * e];
+                if (GATED) u[k][e] = (float)a.up_codes[at + 8 * e];
+                if (a.dy) d[k][e] = load1(dy + 8 * e);
+            }
         }
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-            if (!in[k]) continue;
-            float dx = v[k];
-            if (a.dy) {
-                float f = v[k], slope = 1.f;
-                switch (a.act) {
-                    case OGQ_ACT_RELU: f = act_both<OGQ_ACT_RELU, kAccurate>(f, slope); break;
-                    case OGQ_ACT_SILU: f = act_both<OGQ_ACT_SILU, kAccurate>(f, slope); break;
-                    case OGQ_ACT_GELU: f = act_both<OGQ_ACT_GELU, kAccurate>(f, slope); break;
+            E* out = (E*)a.dx + row[k] * a.ld_dx + col[k];
+            E* dup = (E*)a.dup + row[k] * a.ld_dup + col[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (e >= n[k]) break;
+                const float x = v[k][e] * unit[k];
+                float dx = x;
+                if (a.dy) {
+                    float f = x, slope = 1.f;
+                    switch (a.act) {
+                        case OGQ_ACT_RELU: f = act_both<OGQ_ACT_RELU, kAccurate>(x, slope); break;
+                        case OGQ_ACT_SILU: f = act_both<OGQ_ACT_SILU, kAccurate>(x, slope); break;
+                        case OGQ_ACT_GELU: f = act_both<OGQ_ACT_GELU, kAccurate>(x, slope); break;
+                    }
+                    dx = d[k][e];
+                    if (GATED) {
+                        dx *= u[k][e] * up_unit[k];
+                        store1(dup + 8 * e, d[k][e] * f);
+                    }
+                    dx *= slope;
                 }
-                dx = d[k];
-                if (GATED) {
-                    dx *= u[k];
-                    store1((E*)a.dup + row[k] * a.ld_dup + col[k], d[k] * f);
-                }
-                dx *= slope;
+                store1(out + 8 * e, dx);
             }
-            store1((E*)a.dx + row[k] * a.ld_dx + col[k], dx);
         }
     }
 }
@@ -164,8 +181,8 @@ cudaError_t launch_act8_backward(const Act8Backward& p, int sm_count, cudaStream
             });
         });
     } else {
-        const int64_t want = ((int64_t)a.all_groups + kWarps * 4 - 1) / (kWarps * 4);
-        const int ctas = (int)(want < (int64_t)sm_count * 8 ? want : (int64_t)sm_count * 8);
+        const int64_t want = ((int64_t)a.all_groups + kThreads / 4 - 1) / (kThreads / 4);
+        const int ctas = (int)(want < (int64_t)sm_count * kAct8Ctas ? want : (int64_t)sm_count * kAct8Ctas);
         e = with_dtype(p.dtype, [&](auto elem) {
             return with_bool(p.dup != nullptr, [&](auto gated) {
                 return launch_pdl(k_act8_backward_any<decltype(elem), decltype(gated)::value>, ctas, kThreads, 0, stream, a);
