@@ -32,7 +32,8 @@ constexpr int kWgThreads = 640;                // a warpgroup for TMA, MMA, TMEM
 constexpr int kRegsStart = 96, kRegsControl = 64, kRegsConvert = 56, kRegsSums = 152;
 static_assert(128 * kRegsControl + 256 * kRegsConvert + 256 * kRegsSums <= kWgThreads * kRegsStart, "a warpgroup would wait for registers for ever");
 constexpr uint32_t kTmemColumns = 512;
-constexpr int kMinSteps = 4;                   // fewer steps than these are not split: a second launch costs more than they do
+constexpr int kMinSteps = 4;                   // of a part of a tile, and
+constexpr int kMinSaved = 6;                   // steps that splitting has to save each pair: joining the parts takes 5 us, a step 0.9
 
 template <int BN> struct WgShape {
     static constexpr int kCols = BN / 2;                          // columns of x^ that one CTA converts
@@ -713,15 +714,26 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_bias(const __grid_constant__
     }
 }
 
+// Many chunks: a CTA joins 32 columns, eight chunks at a time.
 __global__ void __launch_bounds__(kThreads) k_wgrad_bias_join(const __grid_constant__ WgBias a)
 {
     pdl_wait();
     pdl_launch_dependents();
-    const int64_t o = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (o >= a.out_cols) return;
-    double s = 0.0;
-    for (int k = 0; k < a.chunks; ++k) s += (double)__ldcg(a.part + k * bias_pitch(a.out_cols) + o);
-    a.db[o] = a.accumulate ? (float)((double)a.db[o] + s) : (float)s;
+    __shared__ float sh[kWarps][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t o = (int64_t)blockIdx.x * 32 + lane;
+    float s = 0.f;
+    if (o < a.out_cols) {
+#pragma unroll 8
+        for (int k = warp; k < a.chunks; k += kWarps) s = __fadd_rn(s, __ldcg(a.part + k * bias_pitch(a.out_cols) + o));
+    }
+    sh[warp][lane] = s;
+    __syncthreads();
+    if (warp || o >= a.out_cols) return;
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) s = __fadd_rn(s, sh[w][lane]);
+    a.db[o] = a.accumulate ? a.db[o] + s : s;
 }
 
 // All sums empty.
@@ -743,6 +755,7 @@ namespace {
 
 constexpr int64_t kLayoutBytes = (int64_t)40 << 20;  // of operands laid out at a time: they stay in L2 until they are read
 constexpr int kBiasCtas = 4;                         // per SM
+constexpr int kBiasParts = 40;                       // up to these are joined by the product's kernel
 constexpr int64_t kBiasRows = 64;                    // up to these, no kernel of its own
 
 int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -829,8 +842,8 @@ cudaError_t launch_product(const CUtensorMap& map_dy, const CUtensorMap& map_x, 
     const int64_t left = tiles - (int64_t)a.whole * a.pairs;
     a.rest = left * a.steps;
     a.per = (a.rest + a.pairs - 1) / a.pairs;
-    if (a.per < kMinSteps) a.per = a.steps < kMinSteps ? a.steps : kMinSteps;
-    if (left == 0) a.per = a.steps;
+    if (a.per < kMinSteps) a.per = kMinSteps;
+    if (left == 0 || a.per + kMinSaved > a.steps) a.per = a.steps;
     const int64_t busy = a.whole ? a.pairs : (a.rest + a.per - 1) / a.per;
     // A build whose kernel starts with fewer registers than the split needs would wait for them for ever: it is not launched.
     static const bool starts_with_all = [] {
@@ -909,6 +922,8 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
     const bool narrow = p.cols <= 128;
     const bool tma_scales = act8_groups(p.cols) % 16 == 0 && (lay_s || ((uintptr_t)p.scales & 15) == 0);
     const bool beside = p.db && p.cols > 0 && p.rows <= kBiasRows && p.dtype == OGQ_BF16;
+    // few parts are joined by the product's kernel; one thread's loop over hundreds would hold it up (100,000 x 8 x 8: 62 us)
+    const bool joined_there = p.cols > 0 && plan.bias_chunks > 1 && plan.bias_chunks <= kBiasParts;
     if (p.db && !beside) {
         const int size = p.dtype == OGQ_F32 ? 4 : 2;
         const bool vec = ((uintptr_t)p.dy & 15) == 0 && p.ld_dy * size % 16 == 0 && p.ld_dy % 8 == 0 && p.out_cols % 8 == 0;
@@ -921,9 +936,9 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
                        : launch_pdl(k_wgrad_bias<E, 1>, b.ctiles * b.chunks, kThreads, 0, stream, b);
         });
         launch_end(stream);
-        if (e == cudaSuccess && b.chunks > 1 && p.cols == 0) {
+        if (e == cudaSuccess && b.chunks > 1 && !joined_there) {
             launch_begin("k_wgrad_bias_join", stream);
-            e = launch_pdl(k_wgrad_bias_join, (int)((p.out_cols + kThreads - 1) / kThreads), kThreads, 0, stream, b);
+            e = launch_pdl(k_wgrad_bias_join, (int)((p.out_cols + 31) / 32), kThreads, 0, stream, b);
             launch_end(stream);
         }
         if (e != cudaSuccess) return e;
@@ -975,7 +990,7 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
         a.last_rows = (int)up_to(rows - (int64_t)(a.steps_x - 1) * kStepRows, 16);
         a.accumulate = acc || t > 0;
         a.db = nullptr;
-        if (t == 0 && (beside || (p.db && plan.bias_chunks > 1))) {
+        if (t == 0 && (beside || (p.db && joined_there))) {
             a.db = p.db;
             a.bias_parts = bias_part;
             a.chunks = beside ? 0 : plan.bias_chunks;
