@@ -43,7 +43,8 @@ template <int BN> struct WgShape {
     static constexpr int kBBytes = kCols * kStepRows * 2;
     static constexpr int kRawBytes = kCols * kStepRows;
     static constexpr int kStages = BN == 256 ? 3 : 4;             // as many as fit: loads under way
-    static constexpr int kSmem = kStages * (kABytes + kRawBytes + kScaleBytes) + kOperands * kBBytes + 1024;  // + alignment to the swizzle's 1024 bytes
+    static constexpr int kRing = kStages * (kABytes + kRawBytes + kScaleBytes) + kOperands * kBBytes;
+    static constexpr int kSmem = kRing + 8 * 32 * 9 * 4 + 1024;    // + patches of rows on their way out, + alignment to the swizzle's 1024 bytes
     static_assert(kABytes % 1024 == 0 && kBBytes % 1024 == 0, "the swizzle goes by the address");
     static_assert(kSmem <= 226 * 1024, "shared memory");
     static constexpr int kSlotFloats = 128 * BN;                  // a partial tile of one CTA
@@ -175,23 +176,37 @@ __device__ __forceinline__ void store8_wide(float* p, const float* v)
                  :: "l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
 
-// Eight neighbouring weights of row o from column i on.
+// Eight neighbouring weights of row o from column i on; cols is a multiple of 8 and rows begin on 32-byte boundaries.
 __device__ __forceinline__ void wg_store8(const WgArgs& a, int64_t o, int64_t i, float (&v)[8])
 {
     if (o >= a.out_cols || i >= a.cols) return;
     float* w = a.dw + o * a.cols + i;
-    if (a.wide) {  // cols is a multiple of 8
-        if (a.accumulate) {
-            const float4 p = *reinterpret_cast<const float4*>(w), q = *reinterpret_cast<const float4*>(w + 4);
-            v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
-            v[4] += q.x; v[5] += q.y; v[6] += q.z; v[7] += q.w;
-        }
-        store8_wide(w, v);
-        return;
+    if (a.accumulate) {
+        const float4 p = *reinterpret_cast<const float4*>(w), q = *reinterpret_cast<const float4*>(w + 4);
+        v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
+        v[4] += q.x; v[5] += q.y; v[6] += q.z; v[7] += q.w;
     }
+    store8_wide(w, v);
+}
+
+// The same for any cols and address, by a warp: lane l has row o + l.  Through shared memory, so that eight lanes write a row's eight
+// weights (300 x 999 x 2001: 35 -> 21 us).
+constexpr int kPatch = 32 * 9;  // floats of a warp
+__device__ __forceinline__ void wg_store_patch(const WgArgs& a, float* patch, int64_t o, int64_t i, const float* v, int lane)
+{
+    __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (i + j < a.cols) w[j] = a.accumulate ? w[j] + v[j] : v[j];
+    for (int j = 0; j < 8; ++j) patch[lane * 9 + j] = v[j];
+    __syncwarp();
+    const int64_t c = i + (lane & 7);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int64_t r = o + k * 4 + (lane >> 3);
+        if (r >= a.out_cols || c >= a.cols) continue;
+        float* w = a.dw + r * a.cols + c;
+        const float x = patch[(k * 4 + (lane >> 3)) * 9 + (lane & 7)];
+        *w = a.accumulate ? *w + x : x;
+    }
 }
 
 // Four lanes with four eights of values each: lane j's eight r becomes lane r's eight j.
@@ -265,7 +280,8 @@ __device__ __forceinline__ void wg_bias(const WgArgs& a, int64_t o)
         if (o + j < a.out_cols) a.db[o + j] = a.accumulate ? a.db[o + j] + sum[j] : sum[j];
 }
 
-template <int BN>
+// WIDE: rows of dW are whole 32-byte pieces
+template <int BN, bool WIDE>
 __global__ void __launch_bounds__(kWgThreads, 1) __cluster_dims__(2, 1, 1)
 k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x,
         const __grid_constant__ CUtensorMap map_scales, const __grid_constant__ WgArgs a)
@@ -504,18 +520,26 @@ k_wgrad(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUte
             wg_tile_place(w.tile, a.tiles_m, a.tiles_n, m, n);
             const int row = quarter * 32 + lane;
             if (w.slot < 0) {
-                // Four lanes exchange their rows' eights of columns, so that they write 128 bytes of one row at a time (a row a lane, 32
-                // bytes at a time: 4.1 us for a tile).
-                const int64_t o = (int64_t)m * kTileM + rank * 128 + (row & ~3), i = (int64_t)n * BN + half * kHalf + (lane & 3) * 8;
+                if constexpr (!WIDE) {
+                    float* patch = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + S::kRing) + (warp - 12) * kPatch;
+                    const int64_t o = (int64_t)m * kTileM + rank * 128 + quarter * 32, i = (int64_t)n * BN + half * kHalf;
 #pragma unroll
-                for (int c = 0; c < kHalf; c += 32) {
-                    wg_exchange(acc + c, lane);
+                    for (int c = 0; c < kHalf; c += 8)
+                        if (i + c < a.cols) wg_store_patch(a, patch, o, i + c, acc + c, lane);
+                } else {
+                    // Four lanes exchange their rows' eights of columns, so that they write 128 bytes of one row at a time (a row a lane, 32
+                    // bytes at a time: 4.1 us for a tile).
+                    const int64_t o = (int64_t)m * kTileM + rank * 128 + (row & ~3), i = (int64_t)n * BN + half * kHalf + (lane & 3) * 8;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float v[8];
+                    for (int c = 0; c < kHalf; c += 32) {
+                        wg_exchange(acc + c, lane);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = acc[c + r * 8 + j];
-                        wg_store8(a, o + r, i + c, v);
+                        for (int r = 0; r < 4; ++r) {
+                            float v[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] = acc[c + r * 8 + j];
+                            wg_store8(a, o + r, i + c, v);
+                        }
                     }
                 }
             } else {
@@ -542,6 +566,7 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_join(const __grid_constant__
     pdl_launch_dependents();
     constexpr int kRows = kThreads / PARTS;  // of the tile's 256 x BN/8 pieces (CTA-of-the-pair, octet, row)
     __shared__ float4 sh[PARTS > 1 ? PARTS : 1][PARTS > 1 ? kRows : 1][2];
+    __shared__ float patches[kRows / 32][kPatch];
     constexpr int kPerTile = 256 * (BN / 8) / kRows;
     const int j = blockIdx.x / kPerTile;
     const int part = threadIdx.x / kRows, r = threadIdx.x - part * kRows;
@@ -586,7 +611,9 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_join(const __grid_constant__
             v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
         }
     }
-    wg_store8(a, (int64_t)m * kTileM + rank * 128 + row, (int64_t)n * BN + oct * 8, v);
+    const int64_t o = (int64_t)m * kTileM + rank * 128 + row, i = (int64_t)n * BN + oct * 8;
+    if (a.wide) wg_store8(a, o, i, v);
+    else wg_store_patch(a, patches[r / 32], o - r % 32, i, v, r % 32);  // (a warp has 32 rows in a row)
 }
 
 // ---------------------------------------------------------------------------
@@ -847,11 +874,13 @@ cudaError_t launch_product(const CUtensorMap& map_dy, const CUtensorMap& map_x, 
     const int64_t busy = a.whole ? a.pairs : (a.rest + a.per - 1) / a.per;
     // A build whose kernel starts with fewer registers than the split needs would wait for them for ever: it is not launched.
     static const bool starts_with_all = [] {
-        cudaFuncAttributes f;
-        return cudaFuncGetAttributes(&f, k_wgrad<BN>) == cudaSuccess && f.numRegs >= kRegsStart;
+        cudaFuncAttributes f, g;
+        return cudaFuncGetAttributes(&f, k_wgrad<BN, false>) == cudaSuccess && f.numRegs >= kRegsStart &&
+               cudaFuncGetAttributes(&g, k_wgrad<BN, true>) == cudaSuccess && g.numRegs >= kRegsStart;
     }();
     if (!starts_with_all) return cudaErrorInvalidConfiguration;
-    cudaError_t e = cudaFuncSetAttribute(k_wgrad<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, WgShape<BN>::kSmem);
+    const auto kernel = a.wide ? k_wgrad<BN, true> : k_wgrad<BN, false>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WgShape<BN>::kSmem);
     if (e != cudaSuccess) return e;
     launch_begin("k_wgrad", stream);
     cudaLaunchAttribute attr;
@@ -864,7 +893,7 @@ cudaError_t launch_product(const CUtensorMap& map_dy, const CUtensorMap& map_x, 
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, k_wgrad<BN>, map_dy, map_x, map_scales, a);
+    e = cudaLaunchKernelEx(&cfg, kernel, map_dy, map_x, map_scales, a);
     launch_end(stream);
     if (e != cudaSuccess || left == 0 || a.per % a.steps == 0) return e;  // no tile is split
     launch_begin("k_wgrad_join", stream);
