@@ -309,7 +309,8 @@ ogq_status ogq_bucket_decode_sum(const uint32_t *const *d_packed_k, const float 
  * Matrices of activations have a row stride ld (in elements, at least cols); columns beyond cols are not touched.  Pointers need the
  * alignment of their type only; calls with pointers on 16-byte boundaries (codes: 8), and cols and strides that are multiples of 8, are faster.
  * Outputs must not overlap inputs, except that d_y may be d_x and d_dx may be d_dy (same stride).  rows * ogq_act8_groups(cols)
- * must be below 2^31 (OGQ_ERR_UNSUPPORTED).  rows = 0 or cols = 0 is allowed and writes nothing.
+ * must be below 2^31 (OGQ_ERR_UNSUPPORTED).  rows = 0 or cols = 0 is allowed and writes nothing.  Calls that may overlap on the GPU
+ * (other streams, graphs replayed side by side) need scratch of their own where they take any.
  *
  *   ogq_act8_encode / ogq_act8_decode: a matrix into this form and back.  A value beyond the range of fp16 decodes to an infinity there.
  *   ogq_act8_forward: y = f(x), or f(x) * up when d_up is given; keeps x (and up) in 8 bits.

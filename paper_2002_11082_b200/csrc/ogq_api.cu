@@ -70,7 +70,7 @@ bool select_size_ok(int64_t total_elems) { return total_elems < ((int64_t)1 << 3
 
 extern "C" {
 
-const char* ogq_version(void) { return "ogq 0.2 (sm_100a)"; }
+const char* ogq_version(void) { return "ogq 0.3 (sm_100a)"; }
 
 unsigned long long ogq_launch_count(void) { return ogq::g_launches.load(std::memory_order_relaxed); }
 

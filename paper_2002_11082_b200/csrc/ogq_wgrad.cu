@@ -934,7 +934,7 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
         launch_end(stream);
         return e;
     }
-    const bool lay_dy = p.dtype != OGQ_BF16 || ((uintptr_t)p.dy & 15) || p.ld_dy % 8;
+    const bool lay_dy = p.dtype != OGQ_BF16 || ((uintptr_t)p.dy & 15) || p.ld_dy % 8 || p.ld_dy >= (int64_t)1 << 39;  // (a tensor map's limit)
     const bool lay_x = ((uintptr_t)p.codes & 15) || p.cols % 16;
     const bool lay_s = ((uintptr_t)p.scales & 3) != 0;
     const Plan plan = make_plan(p.rows, p.cols, p.out_cols, p.dtype, lay_dy, lay_x, lay_s, sm_count);
