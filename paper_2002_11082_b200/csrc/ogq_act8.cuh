@@ -201,7 +201,7 @@ __device__ __forceinline__ void act8_values(uint2 c, float unit, float (&v)[8])
 // ---------------------------------------------------------------------------
 // Activation functions, with the hardware's approximate exponential and reciprocal (2^-22 and 2^-23; the argument's rounding adds
 // |z| 2^-24).  Phi, the normal distribution function, from 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2:
-//   ACCURATE (fp32 activations): the Chebyshev fit of Numerical Recipes' erfcc, erfc(x) = t exp(-x^2 + p(t)), t = 1 / (1 + x / 2), p of
+//   ACCURATE (fp32 activations): the Chebyshev fit in Press et al., Numerical Recipes, section 6.2, erfc(x) = t exp(-x^2 + p(t)), t = 1 / (1 + x / 2), p of
 //   degree 9, off by at most 1.2e-7 of the value, far tails included.  (CUDA's erfcf and expf: 54 us for the forward pass of
 //   group norm with GELU on 16.8 M fp32 values that is bound by memory at 30.)
 //   Otherwise (results rounded to 8 or 11 bits): Abramowitz and Stegun 7.1.26, erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2),

