@@ -342,8 +342,8 @@ ogq_status ogq_act8_backward(const void *d_dy, int64_t ld_dy, const int8_t *d_co
  *   dW[o][i] = sum_t dy[t][o] x^[t][i],   db[o] = sum_t dy[t][o],   t < rows, i < cols, o < out_cols.
  * d_dy [rows, out_cols] of type dtype with row stride ld_dy; d_dw fp32 [out_cols, cols], contiguous; d_db fp32 [out_cols] or NULL.
  * accumulate = 0: the outputs are overwritten; 1: the sums are added to what they hold.  rows = 0 gives sums of 0.
- * Products are exact and sums are fp32; the order of the additions depends on the sizes and the number of SMs only, so the same call
- * gives the same bits again.  d_ws: scratch of ogq_act8_wgrad_workspace_bytes (a size for the current device), 256-byte aligned.
+ * Products are exact and sums are fp32; the order of the additions depends on the sizes, the type, the alignment of the addresses and the
+ * number of SMs only, so the same call gives the same bits again.  d_ws: scratch of ogq_act8_wgrad_workspace_bytes (a size for the current device), 256-byte aligned.
  */
 size_t ogq_act8_wgrad_workspace_bytes(int64_t rows, int64_t cols, int64_t out_cols, int dtype);
 ogq_status ogq_act8_wgrad(const void *d_dy, int64_t ld_dy, const int8_t *d_codes, const uint8_t *d_scales,

@@ -99,6 +99,8 @@ struct Wgrad8 {
 };
 size_t ws_bytes_act8_wgrad(int64_t rows, int64_t cols, int64_t out_cols, int dtype, int sm_count);
 cudaError_t launch_act8_wgrad(const Wgrad8& a, int sm_count, cudaStream_t stream);
+bool act8_wgrad_is_small(const Wgrad8& a, bool more_launches);  // one launch without the tensor cores is faster
+cudaError_t launch_act8_wgrad_small(const Wgrad8& a, cudaStream_t stream);
 
 struct GroupNorm {
     const void* x;             // forward; backward from x itself

@@ -938,6 +938,7 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
     const bool lay_dy = p.dtype != OGQ_BF16 || ((uintptr_t)p.dy & 15) || p.ld_dy % 8 || p.ld_dy >= (int64_t)1 << 39;  // (a tensor map's limit)
     const bool lay_x = ((uintptr_t)p.codes & 15) || p.cols % 16;
     const bool lay_s = ((uintptr_t)p.scales & 3) != 0;
+    if (act8_wgrad_is_small(p, lay_dy || lay_x || lay_s || (p.db && p.rows > kBiasRows))) return launch_act8_wgrad_small(p, stream);
     const Plan plan = make_plan(p.rows, p.cols, p.out_cols, p.dtype, lay_dy, lay_x, lay_s, sm_count);
     char* ws = (char*)p.ws;
     float* slots = (float*)ws;

@@ -13,6 +13,11 @@ SHAPES = [(1, 1, 1), (1, 64, 128), (7, 33, 5), (31, 40, 72), (64, 64, 128), (65,
           (33, 1000, 1000), (200, 17, 1024), (200, 1032, 24), (3000, 128, 136), (5, 4104, 64)]
 
 
+# the same with more rows or weights than one launch takes without the tensor cores
+LARGER = [(2049, 130, 70), (4100, 1, 1), (2500, 17, 24), (700, 333, 999), (64, 1000, 1100), (1, 1032, 1040), (130, 1100, 1300), (513, 96, 130), (2177, 260, 513),
+          (33, 1100, 1001), (6000, 64, 250)]
+
+
 def kept_matrix(gen, rows, cols):
     codes = torch.randint(-127, 128, (rows, cols), device="cuda", generator=gen, dtype=torch.int8)
     scales = torch.randint(115, 124, (rows, -(-cols // 32)), device="cuda", generator=gen).to(torch.uint8)
@@ -48,7 +53,7 @@ def check(dy, x, dw, db, before_w=0.0, before_b=0.0):
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))
-@pytest.mark.parametrize("rows,cols,out", SHAPES)
+@pytest.mark.parametrize("rows,cols,out", SHAPES + LARGER)
 @pytest.mark.parametrize("extra,shift", [(0, 0), (8, 0), (3, 1)])
 def test_against_the_sums(dtype, rows, cols, out, extra, shift):
     d, dt = DTYPES[dtype]
