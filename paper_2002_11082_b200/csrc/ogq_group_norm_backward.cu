@@ -269,10 +269,13 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 3 : 2) k_gn_backward(const 
         float2 t = sh_cta[c];
         if (s.cluster > 1) {
             t = make_float2(0.f, 0.f);
-            for (int r = 0; r < s.cluster; ++r) {
-                const float2 e = gn_remote(&sh_cta[c], r);
-                t.x += e.x;
-                t.y += e.y;
+            float2 e[kGnMaxCluster];  // all under way before the first is added
+#pragma unroll
+            for (int r = 0; r < kGnMaxCluster; ++r) e[r] = r < s.cluster ? gn_remote(&sh_cta[c], r) : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int r = 0; r < kGnMaxCluster; ++r) {
+                t.x += e[r].x;
+                t.y += e[r].y;
             }
         }
         const int64_t at = q.c - q.c0 + c;
