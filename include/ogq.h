@@ -344,6 +344,7 @@ ogq_status ogq_act8_backward(const void *d_dy, int64_t ld_dy, const int8_t *d_co
  * accumulate = 0: the outputs are overwritten; 1: the sums are added to what they hold.  rows = 0 gives sums of 0.
  * Products are exact and sums are fp32; the order of the additions depends on the sizes, the type, the alignment of the addresses and the
  * number of SMs only, so the same call gives the same bits again.  d_ws: scratch of ogq_act8_wgrad_workspace_bytes (a size for the current device), 256-byte aligned.
+ * Should a wait inside the kernel run out (four seconds), its part of the outputs is NaN.
  */
 size_t ogq_act8_wgrad_workspace_bytes(int64_t rows, int64_t cols, int64_t out_cols, int dtype);
 ogq_status ogq_act8_wgrad(const void *d_dy, int64_t ld_dy, const int8_t *d_codes, const uint8_t *d_scales,

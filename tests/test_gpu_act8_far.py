@@ -186,3 +186,24 @@ def test_group_norm_keeps_what_the_encoder_keeps(dtype, N, P, C, G):
         ogq.ogq_group_norm_forward(x, N, P, C, G, d, None, None, 1e-5, ogq.OGQ_ACT_GELU, rounding, 77, 1, y, mean, rstd, *a, ws, ws.numel())
         ogq.ogq_act8_encode(x, C, N * P, C, d, rounding, 77, 1, *b)
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("N,P,C,G", [(2, 9000, 32, 4), (1, 30, 64, 8), (3, 50, 40, 8)])
+def test_group_norm_with_codes_at_an_odd_address(N, P, C, G):
+    """The same results as with aligned codes: forward bit for bit, backward up to the order of the additions."""
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    x, dy = (torch.randn(N * P, C, device="cuda", generator=gen).bfloat16() for _ in range(2))
+    ws = torch.empty(ogq.ogq_group_norm_workspace_bytes(N, P, C, G), dtype=torch.uint8, device="cuda")
+    got = []
+    for shift in (0, 1):
+        flat, bytes_ = torch.zeros(N * P * C + 16, dtype=torch.int8, device="cuda"), torch.zeros(N * P * 2 + 16, dtype=torch.uint8, device="cuda")
+        codes, scales = flat[shift:shift + N * P * C], bytes_[shift:shift + N * P * (-(-C // 32))]
+        y, dx, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(N, G, device="cuda"), torch.empty(N, G, device="cuda")
+        dg, db = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+        ogq.ogq_group_norm_forward(x, N, P, C, G, BF, None, None, 1e-5, ogq.OGQ_ACT_SILU, 0, 0, 0, y, mean, rstd, codes, scales, ws, ws.numel())
+        ogq.ogq_group_norm_backward(dy, None, codes, scales, N, P, C, G, BF, None, None, ogq.OGQ_ACT_SILU, mean, rstd, dx, dg, db, ws, ws.numel())
+        got.append((codes.clone(), scales.clone(), y, dx, dg, db))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    for i, tol in ((2, 2.0 ** -7), (3, 2.0 ** -6), (4, 1e-4), (5, 1e-4)):
+        a, b = got[0][i].float(), got[1][i].float()
+        assert float((a - b).abs().max()) <= tol * (float(a.abs().max()) + 1), i

@@ -152,3 +152,15 @@ def test_bias_beside_the_product(dtype, rows, cols, out):
     w0, b0 = dw.t.clone(), db.t.clone()
     run(dy.t, ld, codes, scales, rows, cols, out, d, 1, dw, db)
     check(dy.t, x, dw, db, w0.double(), b0[0].double())
+
+
+@pytest.mark.parametrize("rows,cols,out", [(700, 512, 700), (3000, 100, 300), (40, 96, 64), (2300, 48, 40)])
+@pytest.mark.parametrize("code_shift,scale_shift", [(1, 0), (0, 1), (16, 4), (3, 2)])
+def test_codes_and_scales_at_any_address(rows, cols, out, code_shift, scale_shift):
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    codes, scales = kept_matrix(gen, rows, cols)
+    c = Guarded(rows, cols, cols, torch.int8, code_shift, codes)
+    s = Guarded(rows, scales.shape[1], scales.shape[1], torch.uint8, scale_shift, scales)
+    dy = torch.randn(rows, out, device="cuda", generator=gen).bfloat16()
+    dw, db = run(dy, out, c.t, s.t, rows, cols, out, ogq.OGQ_BF16)
+    check(dy, decoded(codes, scales), dw, db)
