@@ -16,11 +16,10 @@ struct BwdArgs {
     uint32_t groups;      // of a row
     uint32_t all_groups;  // of the matrix
     uint32_t div_mul, div_shift;  // g / groups = hi(g * div_mul) >> div_shift
-    int act;              // of the kernel of single elements
 };
 
 // Any sizes, strides and addresses: eight lanes a group, elements l, l + 8, l + 16, l + 24 of it for lane l, two groups a lane under way.
-template <class E, bool GATED>
+template <class E, int ACT, bool GATED, bool DECODE>
 __global__ void __launch_bounds__(kThreads) k_act8_backward_any(const __grid_constant__ BwdArgs a)
 {
     pdl_wait();
@@ -33,14 +32,14 @@ __global__ void __launch_bounds__(kThreads) k_act8_backward_any(const __grid_con
     for (uint32_t g0 = blockIdx.x * (kTeams * kUnits) + team; g0 < a.all_groups; g0 += gridDim.x * (kTeams * kUnits)) {
         float v[kUnits][4], u[kUnits][4], d[kUnits][4], unit[kUnits], up_unit[kUnits];
         uint32_t row[kUnits];
-        int64_t col[kUnits];
-        int n[kUnits];  // of this lane's four elements
+        int col[kUnits], n[kUnits];  // first column, how many of this lane's four elements
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
             const uint32_t g = g0 + k * kTeams;
             row[k] = act8_row(a, g);
-            col[k] = (int64_t)(g - row[k] * a.groups) * kAct8Group + l;
-            n[k] = g < a.all_groups ? (int)(a.cols - col[k] >= 25 ? 4 : a.cols > col[k] ? (a.cols - col[k] + 7) / 8 : 0) : 0;
+            col[k] = (int)(g - row[k] * a.groups) * kAct8Group + l;
+            const int left = (int)a.cols - col[k];
+            n[k] = g >= a.all_groups || left <= 0 ? 0 : left >= 25 ? 4 : (left + 7) >> 3;
             const int64_t at = (int64_t)row[k] * a.cols + col[k];
             if (n[k] > 0) {
                 unit[k] = act8_unit(a.scales[g]);
@@ -49,10 +48,11 @@ __global__ void __launch_bounds__(kThreads) k_act8_backward_any(const __grid_con
             const E* dy = (const E*)a.dy + row[k] * a.ld_dy + col[k];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (e >= n[k]) break;
-                v[k][e] = (float)a.codes[at + 8 * e];
-                if (GATED) u[k][e] = (float)a.up_codes[at + 8 * e];
-                if (a.dy) d[k][e] = load1(dy + 8 * e);
+                if (e < n[k]) {
+                    v[k][e] = (float)a.codes[at + 8 * e];
+                    if (GATED) u[k][e] = (float)a.up_codes[at + 8 * e];
+                    if (!DECODE) d[k][e] = load1(dy + 8 * e);
+                }
             }
         }
 #pragma unroll
@@ -61,24 +61,19 @@ __global__ void __launch_bounds__(kThreads) k_act8_backward_any(const __grid_con
             E* dup = (E*)a.dup + row[k] * a.ld_dup + col[k];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (e >= n[k]) break;
                 const float x = v[k][e] * unit[k];
                 float dx = x;
-                if (a.dy) {
-                    float f = x, slope = 1.f;
-                    switch (a.act) {
-                        case OGQ_ACT_RELU: f = act_both<OGQ_ACT_RELU, kAccurate>(x, slope); break;
-                        case OGQ_ACT_SILU: f = act_both<OGQ_ACT_SILU, kAccurate>(x, slope); break;
-                        case OGQ_ACT_GELU: f = act_both<OGQ_ACT_GELU, kAccurate>(x, slope); break;
-                    }
+                if constexpr (!DECODE) {
+                    float slope;
+                    const float f = act_both<ACT, kAccurate>(x, slope);
                     dx = d[k][e];
                     if (GATED) {
                         dx *= u[k][e] * up_unit[k];
-                        store1(dup + 8 * e, d[k][e] * f);
+                        if (e < n[k]) store1(dup + 8 * e, d[k][e] * f);
                     }
                     dx *= slope;
                 }
-                store1(out + 8 * e, dx);
+                if (e < n[k]) store1(out + 8 * e, dx);
             }
         }
     }
@@ -156,7 +151,6 @@ cudaError_t launch_act8_backward(const Act8Backward& p, int sm_count, cudaStream
     a.ld_dy = p.ld_dy; a.ld_dx = p.ld_dx; a.ld_dup = p.ld_dup; a.cols = p.cols;
     a.groups = (uint32_t)act8_groups(p.cols);
     a.all_groups = (uint32_t)(p.rows * a.groups);
-    a.act = p.act;
     const size_t size = p.dtype == OGQ_F32 ? 4 : 2;
     const auto whole = [&](const void* q, int64_t ld) { return ((uintptr_t)q & 15) == 0 && ld * size % 16 == 0; };
     const bool vec = p.cols % 8 == 0 && whole(p.dx, p.ld_dx) && ((uintptr_t)p.codes & 7) == 0 && (!p.dy || whole(p.dy, p.ld_dy)) &&
@@ -185,8 +179,12 @@ cudaError_t launch_act8_backward(const Act8Backward& p, int sm_count, cudaStream
         const int64_t want = ((int64_t)a.all_groups + kThreads / 4 - 1) / (kThreads / 4);
         const int ctas = (int)(want < (int64_t)sm_count * kAct8Ctas ? want : (int64_t)sm_count * kAct8Ctas);
         e = with_dtype(p.dtype, [&](auto elem) {
+            using E = decltype(elem);
+            if (!p.dy) return launch_pdl(k_act8_backward_any<E, OGQ_ACT_NONE, false, true>, ctas, kThreads, 0, stream, a);
             return with_bool(p.dup != nullptr, [&](auto gated) {
-                return launch_pdl(k_act8_backward_any<decltype(elem), decltype(gated)::value>, ctas, kThreads, 0, stream, a);
+                return with_act(p.act, [&](auto act) {
+                    return launch_pdl(k_act8_backward_any<E, decltype(act)::value, decltype(gated)::value, false>, ctas, kThreads, 0, stream, a);
+                });
             });
         });
     }

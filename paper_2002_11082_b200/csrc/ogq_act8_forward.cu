@@ -18,14 +18,13 @@ struct FwdArgs {
     uint32_t all_groups;  // of the matrix
     uint32_t stream_id;
     uint32_t div_mul, div_shift;  // g / groups = hi(g * div_mul) >> div_shift
-    int act;              // of the kernel of single elements
     bool random;
     PhiloxKeys keys;
 };
 
 // Any sizes, strides and addresses: eight lanes a group, elements l, l + 8, l + 16, l + 24 of it for lane l, two groups a lane under way.
 // (A warp per group and a lane per element spent 70 instructions on 32 elements: 4099 x 1001 fp16 11 us.)
-template <class E, bool GATED>
+template <class E, int ACT, bool GATED>
 __global__ void __launch_bounds__(kThreads) k_act8_forward_any(const __grid_constant__ FwdArgs a)
 {
     pdl_wait();
@@ -38,14 +37,14 @@ __global__ void __launch_bounds__(kThreads) k_act8_forward_any(const __grid_cons
     for (uint32_t g0 = blockIdx.x * (kTeams * kUnits) + team; __any_sync(0xffffffffu, g0 < a.all_groups); g0 += gridDim.x * (kTeams * kUnits)) {
         float v[kUnits][4], u[kUnits][4];
         uint32_t row[kUnits];
-        int64_t col[kUnits];
-        int n[kUnits];  // of this lane's four elements
+        int col[kUnits], n[kUnits];  // first column, how many of this lane's four elements
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
             const uint32_t g = g0 + k * kTeams;
             row[k] = act8_row(a, g);
-            col[k] = (int64_t)(g - row[k] * a.groups) * kAct8Group + l;
-            n[k] = g < a.all_groups ? (int)(a.cols - col[k] >= 25 ? 4 : a.cols > col[k] ? (a.cols - col[k] + 7) / 8 : 0) : 0;
+            col[k] = (int)(g - row[k] * a.groups) * kAct8Group + l;
+            const int left = (int)a.cols - col[k];
+            n[k] = g >= a.all_groups || left <= 0 ? 0 : left >= 25 ? 4 : (left + 7) >> 3;
             const E* x = (const E*)a.x + row[k] * a.ld_x + col[k];
             const E* up = (const E*)a.up + row[k] * a.ld_up + col[k];
 #pragma unroll
@@ -74,10 +73,15 @@ __global__ void __launch_bounds__(kThreads) k_act8_forward_any(const __grid_cons
                         const float z = e == 0 ? w[0] : e == 1 ? w[1] : e == 2 ? w[2] : w[3];
                         to[8 * e] = (int8_t)(uint8_t)act8_code_random(z, byte, q == 0 ? r.x : q == 1 ? r.y : q == 2 ? r.z : r.w);
                     }
-                } else {
+                } else if (byte >= kAct8MaxByte) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (e < n[k]) to[8 * e] = (int8_t)(uint8_t)act8_code(w[e], byte);
+                } else {
+                    const float inv = act8_inverse_unit(byte);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < n[k]) to[8 * e] = (int8_t)(uint8_t)__float_as_uint(__fmaf_rn(w[e], inv, 12582912.f));
                 }
                 if (l == 0 && n[k] > 0) (h ? a.up_scales : a.scales)[g0 + k * kTeams] = (uint8_t)byte;
             }
@@ -85,15 +89,9 @@ __global__ void __launch_bounds__(kThreads) k_act8_forward_any(const __grid_cons
                 E* y = (E*)a.y + row[k] * a.ld_y + col[k];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (e >= n[k]) break;
-                    float z = v[k][e];
-                    switch (a.act) {
-                        case OGQ_ACT_RELU: z = act_value<OGQ_ACT_RELU, kAccurate>(z); break;
-                        case OGQ_ACT_SILU: z = act_value<OGQ_ACT_SILU, kAccurate>(z); break;
-                        case OGQ_ACT_GELU: z = act_value<OGQ_ACT_GELU, kAccurate>(z); break;
-                    }
-                    if (GATED) z *= u[k][e];
-                    store1(y + 8 * e, z);
+                    float z = act_value<ACT, kAccurate>(v[k][e]);
+                    if (GATED) z = __fmul_rn(z, u[k][e]);
+                    if (e < n[k]) store1(y + 8 * e, z);
                 }
             }
         }
@@ -170,7 +168,6 @@ cudaError_t launch_act8_forward(const Act8Forward& p, int sm_count, cudaStream_t
     a.groups = (uint32_t)act8_groups(p.cols);
     a.all_groups = (uint32_t)(p.rows * a.groups);
     a.stream_id = p.stream_id;
-    a.act = p.act;
     a.random = p.rounding == OGQ_ROUND_RANDOM;
     a.keys = philox_round_keys((uint32_t)p.seed, (uint32_t)(p.seed >> 32));
     const size_t size = p.dtype == OGQ_F32 ? 4 : 2;
@@ -205,7 +202,9 @@ cudaError_t launch_act8_forward(const Act8Forward& p, int sm_count, cudaStream_t
         const int ctas = (int)(want < (int64_t)sm_count * kAct8Ctas ? want : (int64_t)sm_count * kAct8Ctas);
         e = with_dtype(p.dtype, [&](auto elem) {
             return with_bool(p.up != nullptr, [&](auto gated) {
-                return launch_pdl(k_act8_forward_any<decltype(elem), decltype(gated)::value>, ctas, kThreads, 0, stream, a);
+                return with_act(p.act, [&](auto act) {
+                    return launch_pdl(k_act8_forward_any<decltype(elem), decltype(act)::value, decltype(gated)::value>, ctas, kThreads, 0, stream, a);
+                });
             });
         });
     }
