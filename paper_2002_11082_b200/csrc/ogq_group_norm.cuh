@@ -197,9 +197,9 @@ __device__ __forceinline__ float gn_slope(int act, float z)
     }
 }
 
-// V channels from c on of sample n: z = xh gamma + beta as a multiply-add of centre(x), which is x - mean for fp32 activations
-// (a difference that is exact where x is near the mean) and x itself for 16-bit ones, whose own rounding is 2^-9 or 2^-12 |x|
-// against the 2^-24 |mean| that this adds.
+// V channels from c on of sample n: z = xh gamma + beta as a multiply-add of centre(x).  ACCURATE (fp32 activations, and all sums): x - mean,
+// a difference that is exact where x is near the mean.  Otherwise x itself: a 16-bit x was rounded by 2^-9 or 2^-12 |x|, against
+// the 2^-24 |mean| that this adds.
 template <int V, bool ACCURATE>
 struct GnAffine {
     float mean[ACCURATE ? V : 1], scale[V], shift[V];
@@ -250,13 +250,6 @@ __device__ __forceinline__ void gn_gradient_terms(float2 means, float mean, floa
     offset = -__fmul_rn(rstd, means.x);
     if constexpr (!ACCURATE) offset = __fmaf_rn(-mean, slope, offset);
 }
-// Sum of dz xh from the sums of dz and of dz centre(x).
-template <bool ACCURATE>
-__device__ __forceinline__ float gn_gamma_sum(float dz, float dzx, float mean, float rstd)
-{
-    return __fmul_rn(rstd, ACCURATE ? dzx : __fmaf_rn(-mean, dz, dzx));
-}
-
 // V elements as they lie in memory.
 template <class E, int V> struct GnRaw { E e; };
 template <class E> struct GnRaw<E, 8> { Raw8<E> e; };

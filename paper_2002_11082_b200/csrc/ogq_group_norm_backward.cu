@@ -15,8 +15,8 @@ struct GnPair {
     GnRaw<E, V> dy;
     std::conditional_t<KEPT, GnKept<V>, GnRaw<E, V>> x;
     // dz, and x less the mean or as it is
-    template <int ACT, bool ACCURATE>
-    __device__ __forceinline__ void open(int act, const GnAffine<V, ACCURATE>& f, float (&dz)[V], float (&xc)[V]) const
+    template <int ACT, bool ACCURATE, bool CENTRED>
+    __device__ __forceinline__ void open(int act, const GnAffine<V, CENTRED>& f, float (&dz)[V], float (&xc)[V]) const
     {
         gn_open<E, V>(dy, dz);
         if constexpr (KEPT) gn_open<V>(x, xc);
@@ -55,8 +55,10 @@ struct GnReader {
     }
 };
 
+// Three CTAs an SM for 16-bit types (113.5 us a pass of the shape above, 115.8 with the two that 98 registers leave); fp32 spills at 80
+// registers (4 x 16384 x 256, GELU: 128 us a pass against 116).
 template <class E, int V, int ACT, bool KEPT>
-__global__ void __launch_bounds__(kThreads) k_gn_grad_sums(const __grid_constant__ GnArgs a)
+__global__ void __launch_bounds__(kThreads, sizeof(E) == 4 ? 2 : 3) k_gn_grad_sums(const __grid_constant__ GnArgs a)
 {
     pdl_wait();
     pdl_launch_dependents();
@@ -65,7 +67,7 @@ __global__ void __launch_bounds__(kThreads) k_gn_grad_sums(const __grid_constant
     const GnPlace q = gn_place<V>(a.t);
     if (q.active) {
         const GnReader<E, V, KEPT> in(a, q);
-        GnAffine<V, kAccurate> f;
+        GnAffine<V, true> f;  // sums of dz (x - mean): less the mean first, so that nothing is lost when they cancel
         gn_affine(a, q.n, q.c, f);
         float sb[V], sg[V];
 #pragma unroll
@@ -80,21 +82,21 @@ __global__ void __launch_bounds__(kThreads) k_gn_grad_sums(const __grid_constant
                                               sg[j] = __fmaf_rn(dz[j], xc[j], sg[j]);
                                           }
                                       });
-        gn_channels<V>(a, q.n, q.c, [&](int j, float mean, float rstd, int64_t) {
-            sh[(q.ty * a.t.tx + q.tx) * V + j] = make_float2(sb[j], gn_gamma_sum<kAccurate>(sb[j], sg[j], mean, rstd));
+        gn_channels<V>(a, q.n, q.c, [&](int j, float, float rstd, int64_t) {
+            sh[(q.ty * a.t.tx + q.tx) * V + j] = make_float2(sb[j], __fmul_rn(sg[j], rstd));
         });
     }
     __syncthreads();
     for (int j = threadIdx.x; j < a.t.tx * V; j += kThreads) {
         const int64_t c = (int64_t)q.tile * a.t.tx * V + j;
         if (c >= a.t.C) break;
-        float2 s = make_float2(0.f, 0.f);
+        double s1 = 0.0, s2 = 0.0;  // up to 256 rows, one after the other, of sums that may cancel
         for (int y = 0; y < a.t.ty; ++y) {
             const float2 e = sh[y * a.t.tx * V + j];
-            s.x += e.x;
-            s.y += e.y;
+            s1 += (double)e.x;
+            s2 += (double)e.y;
         }
-        a.part[((int64_t)q.n * a.t.chunks + q.chunk) * a.t.C + c] = s;
+        a.part[((int64_t)q.n * a.t.chunks + q.chunk) * a.t.C + c] = make_float2((float)s1, (float)s2);
     }
 }
 
@@ -222,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 3 : 2) k_gn_backward(const 
             rx[u] = in[u] ? load_raw8((const E*)a.x + row * a.t.C + q.c) : zero_raw8<E>();
         }
     }
-    GnAffine<8, kAccurate> z;
+    GnAffine<8, true> z;
     if (q.active) gn_affine(a, q.n, q.c, z);
     float dz[U][8];
     float2 sum[8];
@@ -245,9 +247,7 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 3 : 2) k_gn_backward(const 
         }
     }
     if (q.active)
-        gn_channels<8>(a, q.n, q.c, [&](int j, float mean, float rstd, int64_t) {
-            sum[j].y = gn_gamma_sum<kAccurate>(sum[j].x, sum[j].y, mean, rstd);
-        });
+        gn_channels<8>(a, q.n, q.c, [&](int j, float, float rstd, int64_t) { sum[j].y = __fmul_rn(sum[j].y, rstd); });
     gn_put_sums(s, q, sum, sh, s.width);
     __syncthreads();
     for (int c = threadIdx.x; c < s.width; c += kThreads) {
@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 3 : 2) k_gn_backward(const 
         float slope[8], offset[8];
         const int64_t base = q.n * a.t.G + (int)(q.c - q.c0) / s.per;  // the slab's first group
         gn_channels<8>(a, q.n, q.c, [&](int j, float mean, float rstd, int64_t at) {
-            gn_gradient_terms<kAccurate>(sh_group[at - base], mean, rstd, slope[j], offset[j]);
+            gn_gradient_terms<true>(sh_group[at - base], mean, rstd, slope[j], offset[j]);
         });
 #pragma unroll
         for (int u = 0; u < U; ++u) {

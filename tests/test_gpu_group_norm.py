@@ -182,6 +182,26 @@ def test_a_mean_far_above_the_deviation(dtype, offset, P, C, G):
     check_forward(c, x, y, ones, zeros, ref.NONE)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("N,P,C,G", [(1, 49, 64, 8), (1, 49, 30, 3), (400, 49, 64, 8)])
+def test_gradient_of_gamma_with_a_mean_far_above_the_deviation(dtype, N, P, C, G):
+    """dgamma = sum dy (x - mean) rstd without a function: the difference is rounded once, the product, the sum's result and its factor once each,
+    and a sum of P values rounds none of them more than P - 1 times, whatever the order; samples are joined in 64 bits.  So P + 8 steps of the
+    sum of magnitudes, and nothing in proportion to |mean| rstd, 1200 (fp16) and 300 (bf16) here."""
+    c = Call(N, P, C, G, dtype)
+    rng = np.random.default_rng(21)
+    step, offset = (1.0, 1040.0) if dtype == "f16" else (1.0, 250.0)
+    x = torch.from_numpy(rng.integers(-1, 2, (N, P, C)) * step + offset).to(c.dt)
+    dy = torch.from_numpy(0.5 + rng.random((N, P, C))).to(c.dt)
+    c.forward(x, None, None, ogq.OGQ_ACT_NONE, keep=False)
+    _, dg, db = c.backward(dy, x, None, None, ogq.OGQ_ACT_NONE)
+    xn, dn = x.double().numpy(), dy.double().numpy()
+    xh = (xn - ref.wide(c.mean.numpy(), C)) * ref.wide(c.rstd.numpy(), C)
+    assert np.abs(ref.wide(c.mean.numpy() * c.rstd.numpy(), C)).min() > 250
+    for got, terms in ((dg, dn * xh), (db, dn)):
+        assert_near(got.numpy()[0], terms.sum(axis=(0, 1)), (P + 8) * U24 * np.abs(terms).sum(axis=(0, 1)), "dgamma, dbeta")
+
+
 def test_constant_groups_and_non_finite_values():
     """Variance 0: rstd is 1 / sqrt(eps) and the outputs are beta.  A NaN or an infinity stays in its group of its sample."""
     N, P, C, G = 2, 40, 64, 8
