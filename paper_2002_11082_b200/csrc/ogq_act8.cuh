@@ -275,7 +275,7 @@ __device__ __forceinline__ float act_slope(float z)
     if constexpr (ACT == OGQ_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
     if constexpr (ACT == OGQ_ACT_SILU) {
         const float s = sigmoid(z), t = __fmul_rn(z, s);
-        return __fmaf_rn(-t, s, __fadd_rn(s, t));
+        return __fmaf_rn(t, __fsub_rn(1.f, s), s);  // (s + t - t s would be 0 where s + t is rounded to t, from 2^24 on)
     }
     if constexpr (ACT == OGQ_ACT_GELU) {
         float e;
@@ -291,7 +291,7 @@ __device__ __forceinline__ float act_both(float z, float& slope)
 {
     if constexpr (ACT == OGQ_ACT_SILU) {
         const float s = sigmoid(z), t = __fmul_rn(z, s);
-        slope = __fmaf_rn(-t, s, __fadd_rn(s, t));
+        slope = __fmaf_rn(t, __fsub_rn(1.f, s), s);
         return t;
     }
     if constexpr (ACT == OGQ_ACT_GELU) {

@@ -1,0 +1,66 @@
+"""The activation functions of the 8-bit activations at large arguments and in relative error, against their definitions in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import act8_reference as ref
+import paper_2002_11082_b200 as ogq
+from act8_gpu import ACTS, DTYPES, kept
+
+pytestmark = pytest.mark.gpu
+
+
+def forward_and_backward(z, dtype, act, cols, up=None, dy=None):
+    """y, dx (and dup) of the values z, one in each group (all else 0), whose kept form is z itself; vector kernels for cols = 64, the others for 33."""
+    d, dt = DTYPES[dtype]
+    a, _ = ACTS[act]
+    n = len(z)
+    put = lambda v: torch.zeros(n, cols, dtype=dt, device="cuda").index_put_((torch.arange(n, device="cuda"), torch.full((n,), 7, device="cuda")), v.cuda().to(dt))  # noqa: E731
+    x, dys = put(z), put(torch.ones(n) if dy is None else dy)
+    ups = None if up is None else put(up)
+    codes, scales = kept(n, cols)
+    up_codes, up_scales = kept(n, cols)
+    g = (ups, cols, up_codes.t, up_scales.t) if up is not None else (None, 0, None, None)
+    y, dx, dup = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    ogq.ogq_act8_forward(x, cols, g[0], g[1], n, cols, d, a, 0, 0, 0, y, cols, codes.t, scales.t, g[2], g[3])
+    ogq.ogq_act8_backward(dys, cols, codes.t, scales.t, g[2], g[3], n, cols, d, a, dx, cols, dup if up is not None else None, cols)
+    unit = (scales.t.int() << 23).view(torch.float32)
+    assert torch.equal(codes.t[:, 7].float() * unit[:, 0], x[:, 7].float()), "these values have a kept form of their own"
+    return y[:, 7], dx[:, 7], dup[:, 7]
+
+
+LARGE = [32.0, 1000.0, 2.0 ** 16 - 512, 2.0 ** 24, 2.0 ** 25, 127 * 2.0 ** 30, 2.0 ** 100, 2.0 ** 126]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("cols", [64, 33])
+def test_slope_of_silu_at_large_arguments(dtype, gated, cols):
+    """From z = 32 on the slope is 1 + z exp(-z) < 1 + 2^-40, f(z) = z (1 - 2^-46): to the last bit dx = dy [up] and dup = dy z.  Below -200 both are 0."""
+    z = torch.tensor(LARGE + [-1000.0, -2.0 ** 25, -2.0 ** 126])
+    dy, up = torch.full((len(z),), 0.75), torch.full((len(z),), -1.5) if gated else None
+    _, dx, dup = forward_and_backward(z, dtype, "silu", cols, up, dy)
+    n = len(LARGE)
+    assert dx[:n].float().tolist() == [0.75 * (-1.5 if gated else 1.0)] * n
+    assert not dx[n:].any()
+    if gated:
+        want = 0.75 * torch.tensor(LARGE).to(DTYPES[dtype][1])
+        assert torch.equal(dup[:n].cpu(), want) and not dup[n:].any()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("P,C,G", [(6, 32, 1), (6, 30, 1), (70000, 32, 4)])
+def test_slope_of_silu_behind_a_large_gamma(dtype, P, C, G):
+    """z = gamma xh beyond 2^24 in magnitude, whose slope is 0 or 1: dbeta counts the positive ones."""
+    d, dt = DTYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = (torch.randint(0, 2, (P, C), device="cuda", generator=gen) * 2 - 1).to(dt) * 4
+    x[0], x[1] = 4, -4
+    gamma = torch.full((C,), 2.0 ** 30, device="cuda")
+    ws = torch.empty(ogq.ogq_group_norm_workspace_bytes(1, P, C, G), dtype=torch.uint8, device="cuda")
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd, dg, db = (torch.empty(n, device="cuda") for n in (G, G, C, C))
+    ogq.ogq_group_norm_forward(x, 1, P, C, G, d, gamma, None, 1e-5, ogq.OGQ_ACT_NONE, 0, 0, 0, y, mean, rstd, None, None, ws, ws.numel())
+    assert bool((mean.abs() < 3.9).all())
+    ogq.ogq_group_norm_backward(torch.ones_like(x), x, None, None, 1, P, C, G, d, gamma, None, ogq.OGQ_ACT_SILU, mean, rstd, dx, dg, db, ws, ws.numel())
+    assert torch.equal(db, (x > 0).sum(0).float())
