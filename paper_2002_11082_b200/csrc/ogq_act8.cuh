@@ -199,12 +199,13 @@ __device__ __forceinline__ void act8_values(uint2 c, float unit, float (&v)[8])
 }
 
 // ---------------------------------------------------------------------------
-// Activation functions, with the hardware's approximate exponential and reciprocal (2^-22 and 2^-23; the argument's rounding adds
-// |z| 2^-24).  Phi, the normal distribution function, from 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2:
-//   ACCURATE (fp32 activations): the Chebyshev fit in Press et al., Numerical Recipes, section 6.2, erfc(x) = t exp(-x^2 + p(t)), t = 1 / (1 + x / 2), p of
-//   degree 9, off by at most 1.2e-7 of the value, far tails included.  (CUDA's erfcf and expf: 54 us for the forward pass of
-//   group norm with GELU on 16.8 M fp32 values that is bound by memory at 30.)
-//   Otherwise (results rounded to 8 or 11 bits): Abramowitz and Stegun 7.1.26, erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2),
+// Activation functions.  ACCURATE (fp32 activations) or for results that are rounded to 8 or 11 bits, with the hardware's approximate exponential and
+// reciprocal (2^-22 and 2^-23; the argument's rounding adds |z| 2^-24).
+// Phi, the normal distribution function, from 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2:
+//   ACCURATE: the Chebyshev fit in Press et al., Numerical Recipes, section 6.2, erfc(x) = t exp(-x^2 + p(t)), t = 1 / (1 + x / 2), p of
+//   degree 9, off by at most 1.2e-7 of the value, far tails included, and z^2 2^-23 from the rounding of the exponential's argument.  (CUDA's erfcf and expf: 54 us
+//   for the forward pass of group norm with GELU on 16.8 M fp32 values that is bound by memory at 30.)
+//   Otherwise: Abramowitz and Stegun 7.1.26, erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2),
 //   t = 1 / (1 + p x), off by at most 1.5e-7, which shares its exponential with the density in the slope.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float fast_exp2(float x)
@@ -221,9 +222,25 @@ __device__ __forceinline__ float fast_reciprocal(float x)
 }
 constexpr float kLog2e = 1.44269504f;
 
-__device__ __forceinline__ float sigmoid(float z)
+// 1 / (1 + exp(-z)), and one less that in `rest`.  ACCURATE: what rounding z log2(e) takes from ex2's argument is made up for (without that f(z) was 3.8e-6 of itself
+// off at z = -80), and the rest comes from the exponential, so that it is not a difference.  From z = 128 on exp(-z) is 0, where it or its correction overflow it is
+// 2^127, whose reciprocal is 0.  (expf and a reciprocal to nearest: 4 x 16384 x 256 with SiLU, forward and backward, 131 us; so 113 us; neither 112.)
+template <bool ACCURATE>
+__device__ __forceinline__ float sigmoid(float z, float& rest)
 {
-    return fast_reciprocal(__fadd_rn(1.f, fast_exp2(__fmul_rn(z, -kLog2e))));
+    if constexpr (ACCURATE) {
+        const float c = fminf(z, 128.f), h = __fmul_rn(c, -kLog2e);
+        const float l = __fmaf_rn(c, -1.92596299e-8f, __fmaf_rn(c, -kLog2e, -h));  // log2(e) less kLog2e
+        const float p = fast_exp2(h);
+        const float e = fminf(__fmaf_rn(p, __fmul_rn(l, 0.693147181f), p), 0x1p127f);
+        const float s = fast_reciprocal(__fadd_rn(1.f, e));
+        rest = __fmul_rn(e, s);
+        return s;
+    } else {
+        const float s = fast_reciprocal(__fadd_rn(1.f, fast_exp2(__fmul_rn(z, -kLog2e))));
+        rest = __fsub_rn(1.f, s);
+        return s;
+    }
 }
 
 // Phi(z), and exp(-z^2/2) in e
@@ -261,7 +278,10 @@ template <int ACT, bool ACCURATE>
 __device__ __forceinline__ float act_value(float z)
 {
     if constexpr (ACT == OGQ_ACT_RELU) return z > 0.f ? z : z == z ? 0.f : z;
-    if constexpr (ACT == OGQ_ACT_SILU) return __fmul_rn(z, sigmoid(z));
+    if constexpr (ACT == OGQ_ACT_SILU) {
+        float rest;
+        return __fmul_rn(z, sigmoid<ACCURATE>(z, rest));
+    }
     if constexpr (ACT == OGQ_ACT_GELU) {
         float e;
         return z * normal_cdf<ACCURATE>(z, e);
@@ -274,8 +294,9 @@ __device__ __forceinline__ float act_slope(float z)
 {
     if constexpr (ACT == OGQ_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
     if constexpr (ACT == OGQ_ACT_SILU) {
-        const float s = sigmoid(z), t = __fmul_rn(z, s);
-        return __fmaf_rn(t, __fsub_rn(1.f, s), s);  // (s + t - t s would be 0 where s + t is rounded to t, from 2^24 on)
+        float rest;
+        const float s = sigmoid<ACCURATE>(z, rest);
+        return __fmaf_rn(__fmul_rn(z, s), rest, s);  // (s + t - t s, t = z s, would be 0 where s + t is rounded to t, from 2^24 on)
     }
     if constexpr (ACT == OGQ_ACT_GELU) {
         float e;
@@ -290,8 +311,9 @@ template <int ACT, bool ACCURATE>
 __device__ __forceinline__ float act_both(float z, float& slope)
 {
     if constexpr (ACT == OGQ_ACT_SILU) {
-        const float s = sigmoid(z), t = __fmul_rn(z, s);
-        slope = __fmaf_rn(t, __fsub_rn(1.f, s), s);
+        float rest;
+        const float s = sigmoid<ACCURATE>(z, rest), t = __fmul_rn(z, s);
+        slope = __fmaf_rn(t, rest, s);
         return t;
     }
     if constexpr (ACT == OGQ_ACT_GELU) {

@@ -5,7 +5,7 @@ import torch
 
 import act8_reference as ref
 import paper_2002_11082_b200 as ogq
-from act8_gpu import ACTS, DTYPES, kept
+from act8_gpu import ACTS, DTYPES, assert_near, kept
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,33 @@ def test_slope_of_silu_behind_a_large_gamma(dtype, P, C, G):
     assert bool((mean.abs() < 3.9).all())
     ogq.ogq_group_norm_backward(torch.ones_like(x), x, None, None, 1, P, C, G, d, gamma, None, ogq.OGQ_ACT_SILU, mean, rstd, dx, dg, db, ws, ws.numel())
     assert torch.equal(db, (x > 0).sum(0).float())
+
+
+def kept_grid(least, most, per):
+    """Values of both signs whose kept form is themselves (at most seven bits), `per` (8 to 64, a power of two) in each power of two."""
+    m = torch.arange(64, 128, 64 // per, dtype=torch.float64)
+    z = torch.cat([m * 2.0 ** e for e in range(-12, 3)])
+    z = z[(z >= least) & (z <= most)]
+    return torch.cat([z, -z])
+
+
+SUBNORMAL = 2.0 ** -149
+
+
+@pytest.mark.parametrize("cols", [64, 33])
+@pytest.mark.parametrize("gated", [False, True])
+def test_silu_in_fp32_relative_to_its_value(cols, gated):
+    """In half steps of fp32 (2^-24): ex2 is off by 4 at most (2^-22), the correction of its argument, 1 + exp, the product with z and a gate's by one each, rcp by 2
+    (one step of 2^-23): 10 of f(z), whatever z.  The slope s + f (1 - s): f by 9 (without the gate), 1 - s = exp s by 5 + 8 + 1, the sum's two roundings are of s + f (1 - s)
+    and s is off by 8, the product with dy and a gate's by one each: 27 of |s| + |f (1 - s)|."""
+    z = kept_grid(2.0 ** -6, 86.0, 64)
+    up = torch.full((len(z),), 1.25) if gated else None
+    y, dx, dup = forward_and_backward(z, "f32", "silu", cols, up)
+    zn = z.double().numpy()
+    f, s = ref.value(ref.SILU, zn), 1 / (1 + np.exp(-zn))
+    g = 1.25 if gated else 1.0
+    h = 2.0 ** -24
+    assert_near(y.double().cpu().numpy(), g * f, 10 * h * g * np.abs(f) + SUBNORMAL, "y")
+    assert_near(dx.double().cpu().numpy(), g * ref.slope(ref.SILU, zn), 27 * h * g * (s + np.abs(f) / (1 + np.exp(zn))) + SUBNORMAL, "dx")
+    if gated:
+        assert_near(dup.double().cpu().numpy(), f, 10 * h * np.abs(f) + SUBNORMAL, "dup")
