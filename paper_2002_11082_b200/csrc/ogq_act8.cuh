@@ -205,8 +205,10 @@ __device__ __forceinline__ void act8_values(uint2 c, float unit, float (&v)[8])
 //   ACCURATE: the Chebyshev fit in Press et al., Numerical Recipes, section 6.2, erfc(x) = t exp(-x^2 + p(t)), t = 1 / (1 + x / 2), p of
 //   degree 9, off by at most 1.2e-7 of the value, far tails included, and z^2 2^-23 from the rounding of the exponential's argument.  (CUDA's erfcf and expf: 54 us
 //   for the forward pass of group norm with GELU on 16.8 M fp32 values that is bound by memory at 30.)
-//   Otherwise: Abramowitz and Stegun 7.1.26, erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2),
-//   t = 1 / (1 + p x), off by at most 1.5e-7, which shares its exponential with the density in the slope.
+//   Otherwise: exp(-z^2/2) (a1 t + ... + a7 t^7), t = 1 / (1 + p |z|), the a's and p of least largest error of exp(z^2/2) (1 - Phi) over |z| <= 13.5 (a linear
+//   program at 3,000 places), relative and allowed to grow with exp(z^2/4) up to ten times: 1.7e-7 of the value off at 0, 1.7e-6 at most.  It shares its exponential with
+//   the density in the slope.  (A fit of five terms bounded in its absolute error only, Abramowitz and Stegun 7.1.26, was 1.6e-3 of the value off at -5, near bf16's half
+//   step of 2e-3, and 5e-4, fp16's, at -4; it takes one instruction less in the slope alone and two elsewhere.)
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float fast_exp2(float x)
 {
@@ -243,11 +245,26 @@ __device__ __forceinline__ float sigmoid(float z, float& rest)
     }
 }
 
+// 1 - Phi(|z|) over e = exp(-z^2/2), the fit of 16-bit types
+__device__ __forceinline__ float normal_tail_over_e(float z)
+{
+    const float t = fast_reciprocal(__fmaf_rn(fabsf(z), 0.259f, 1.f));
+    float p = __fmaf_rn(t, -0.0753390088f, 0.241071129f);
+    p = __fmaf_rn(p, t, -0.122635168f);
+    p = __fmaf_rn(p, t, 0.177393909f);
+    p = __fmaf_rn(p, t, 0.0688966541f);
+    p = __fmaf_rn(p, t, 0.107552936f);
+    p = __fmaf_rn(p, t, 0.103059548f);
+    return __fmul_rn(p, t);
+}
+__device__ __forceinline__ float normal_e(float z) { return fast_exp2(__fmul_rn(__fmul_rn(z, -0.5f * kLog2e), z)); }
+constexpr float kDensity = 0.39894228040143268f;  // 1 / sqrt(2 pi)
+
 // Phi(z), and exp(-z^2/2) in e
 template <bool ACCURATE>
 __device__ __forceinline__ float normal_cdf(float z, float& e)
 {
-    e = fast_exp2(__fmul_rn(__fmul_rn(z, -0.5f * kLog2e), z));
+    e = normal_e(z);
     float tail;
     if constexpr (ACCURATE) {
         const float x = fabsf(z) * 0.70710678118654752f;
@@ -263,12 +280,7 @@ __device__ __forceinline__ float normal_cdf(float z, float& e)
         p = __fmaf_rn(p, t, -1.26551223f);
         tail = __fmul_rn(0.5f * t, fast_exp2(__fmul_rn(__fmaf_rn(-x, x, p), kLog2e)));
     } else {
-        const float t = fast_reciprocal(__fmaf_rn(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
-        float p = __fmaf_rn(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-        p = __fmaf_rn(p, t, 0.5f * 1.421413741f);
-        p = __fmaf_rn(p, t, 0.5f * -0.284496736f);
-        p = __fmaf_rn(p, t, 0.5f * 0.254829592f);
-        tail = __fmul_rn(__fmul_rn(p, t), e);
+        tail = __fmul_rn(normal_tail_over_e(z), e);
     }
     return z < 0.f ? tail : __fsub_rn(1.f, tail);
 }
@@ -299,9 +311,14 @@ __device__ __forceinline__ float act_slope(float z)
         return __fmaf_rn(__fmul_rn(z, s), rest, s);  // (s + t - t s, t = z s, would be 0 where s + t is rounded to t, from 2^24 on)
     }
     if constexpr (ACT == OGQ_ACT_GELU) {
-        float e;
-        const float p = normal_cdf<ACCURATE>(z, e);
-        return __fmaf_rn(z * 0.39894228040143268f, e, p);
+        if constexpr (ACCURATE) {
+            float e;
+            const float p = normal_cdf<true>(z, e);
+            return __fmaf_rn(z * kDensity, e, p);
+        } else {  // Phi and z times the density have the same exponential
+            const float t = __fmul_rn(__fmaf_rn(fabsf(z), -kDensity, normal_tail_over_e(z)), normal_e(z));
+            return z < 0.f ? t : __fsub_rn(1.f, t);
+        }
     }
     return 1.f;
 }
@@ -319,7 +336,7 @@ __device__ __forceinline__ float act_both(float z, float& slope)
     if constexpr (ACT == OGQ_ACT_GELU) {
         float e;
         const float p = normal_cdf<ACCURATE>(z, e);
-        slope = __fmaf_rn(z * 0.39894228040143268f, e, p);
+        slope = __fmaf_rn(z * kDensity, e, p);
         return z * p;
     }
     slope = act_slope<ACT, ACCURATE>(z);

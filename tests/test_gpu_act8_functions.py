@@ -5,7 +5,7 @@ import torch
 
 import act8_reference as ref
 import paper_2002_11082_b200 as ogq
-from act8_gpu import ACTS, DTYPES, assert_near, kept
+from act8_gpu import ACTS, DTYPES, assert_near, half_step, kept, smallest
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +94,22 @@ def test_silu_in_fp32_relative_to_its_value(cols, gated):
     assert_near(dx.double().cpu().numpy(), g * ref.slope(ref.SILU, zn), 27 * h * g * (s + np.abs(f) / (1 + np.exp(zn))) + SUBNORMAL, "dx")
     if gated:
         assert_near(dup.double().cpu().numpy(), f, 10 * h * np.abs(f) + SUBNORMAL, "dup")
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("cols", [64, 33])
+def test_gelu_relative_to_its_value(dtype, cols):
+    """Phi(-|z|) is the fit of a function of t = 1 / (1 + p |z|), 1.7e-6 off at most in 16 bits and 1.2e-7 in fp32, times an exponential.  In half steps of fp32: t is
+    off by 5 (its factor of |z|, the sum, rcp), which the fitted function takes at most 2.5 times; the polynomial's additions, ex2 and the last products make 15 more;
+    the exponential's argument, z^2/2 and in fp32 up to 1.3 more, has been rounded 7 times at most.  So the tail is off by 32 + 7 (z^2/2 + 1.3) half steps and the fit.
+    exp(-z^2/2) is taken as 0 where it is below 2^-126 (z beyond 13.2), which the range leaves out.  The slope Phi + z phi: the same of both terms."""
+    _, dt = DTYPES[dtype]
+    z = kept_grid(2.0 ** -6, 12.5, 64)
+    y, dx, _ = forward_and_backward(z, dtype, "gelu", cols)
+    zn = z.double().numpy()
+    rel = (1.2e-7 if dtype == "f32" else 1.7e-6) + (32 + 7 * (zn ** 2 / 2 + 1.3)) * 2.0 ** -24
+    f, phi = ref.value(ref.GELU, zn), np.abs(zn) * np.exp(-zn ** 2 / 2) / np.sqrt(2 * np.pi)
+    last, low = half_step(dt) * 1.01, smallest(dt) + SUBNORMAL
+    assert_near(y.double().cpu().numpy(), f, (last + rel) * np.abs(f) + low, "y")
+    s = ref.slope(ref.GELU, zn)
+    assert_near(dx.double().cpu().numpy(), s, last * np.abs(s) + rel * (np.abs(f / zn) + phi) + low, "dx")
