@@ -66,12 +66,11 @@ __global__ void __launch_bounds__(kThreads) k_act8_backward_any(const __grid_con
                 if constexpr (!DECODE) {
                     float slope;
                     const float f = act_both<ACT, kAccurate>(x, slope);
-                    dx = d[k][e];
+                    dx = d[k][e] * slope;
                     if (GATED) {
                         dx *= u[k][e] * up_unit[k];
                         if (e < n[k]) store1(dup + 8 * e, d[k][e] * f);
                     }
-                    dx *= slope;
                 }
                 if (e < n[k]) store1(out + 8 * e, dx);
             }
@@ -130,7 +129,7 @@ __global__ void __launch_bounds__(kThreads) k_act8_backward(const __grid_constan
                     for (int j = 0; j < 8; ++j) {
                         float slope;
                         dup[j] = __fmul_rn(d[j], act_both<ACT, kAccurate>(v[j], slope));
-                        d[j] = __fmul_rn(__fmul_rn(d[j], w[j]), slope);
+                        d[j] = __fmul_rn(__fmul_rn(d[j], slope), w[j]);  // (dy up^ alone may be infinite where the slope is 0)
                     }
                     store8((E*)a.dup + row[k] * a.ld_dup + col[k], dup);
                 } else {

@@ -113,3 +113,15 @@ def test_gelu_relative_to_its_value(dtype, cols):
     assert_near(y.double().cpu().numpy(), f, (last + rel) * np.abs(f) + low, "y")
     s = ref.slope(ref.GELU, zn)
     assert_near(dx.double().cpu().numpy(), s, last * np.abs(s) + rel * (np.abs(f / zn) + phi) + low, "dx")
+
+
+@pytest.mark.parametrize("cols", [64, 33])
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+def test_gate_and_gradient_whose_product_alone_overflows(act, cols):
+    """dx = dy f'(x^) up^: where the slope is 0 or tiny, dy up^ alone must not become infinite."""
+    z = torch.tensor([-1.0 if act == "relu" else -100.0, -1.0 if act == "relu" else -200.0])
+    big = torch.full((2,), 2.0 ** 70)
+    _, dx, dup = forward_and_backward(z, "f32", act, cols, big, big)
+    assert bool(torch.isfinite(dx).all()) and bool(torch.isfinite(dup).all())
+    if act == "relu":
+        assert not dx.any()
