@@ -197,27 +197,18 @@ __device__ __forceinline__ float gn_slope(int act, float z)
     }
 }
 
-// V channels from c on of sample n: z = xh gamma + beta as a multiply-add of centre(x).  ACCURATE (fp32 activations, and all sums): x - mean,
-// a difference that is exact where x is near the mean.  Otherwise x itself: a 16-bit x was rounded by 2^-9 or 2^-12 |x|, against
-// the 2^-24 |mean| that this adds.
-template <int V, bool ACCURATE>
+// V channels from c on of sample n: z = xh gamma + beta as a multiply-add of x - mean, a difference that is exact where x is near the mean.  (With the mean in the
+// addend, beta - mean scale, z was off by 2^-24 |mean| rstd: a group of one value, rstd = 316, did not give beta, and the two passes could take different sides of ReLU.)
+template <int V>
 struct GnAffine {
-    float mean[ACCURATE ? V : 1], scale[V], shift[V];
+    float mean[V], scale[V], shift[V];
     __device__ __forceinline__ void set(int j, float m, float rstd, float gamma, float beta)
     {
+        mean[j] = m;
         scale[j] = __fmul_rn(rstd, gamma);
-        if constexpr (ACCURATE) {
-            mean[j] = m;
-            shift[j] = beta;
-        } else {
-            shift[j] = __fmaf_rn(-m, scale[j], beta);
-        }
+        shift[j] = beta;
     }
-    __device__ __forceinline__ float centre(float x, int j) const
-    {
-        if constexpr (ACCURATE) return __fsub_rn(x, mean[j]);
-        return x;
-    }
+    __device__ __forceinline__ float centre(float x, int j) const { return __fsub_rn(x, mean[j]); }
     __device__ __forceinline__ float z(float centred, int j) const { return __fmaf_rn(centred, scale[j], shift[j]); }
 };
 // Calls f(j, mean, rstd, group) for V channels from c on of sample n.
@@ -235,20 +226,18 @@ __device__ __forceinline__ void gn_channels(const GnArgs& a, int64_t n, int64_t 
         f(j, a.mean[at], a.rstd[at], at);  // (from L1 where they are asked for again)
     }
 }
-template <int V, bool ACCURATE>
-__device__ __forceinline__ void gn_affine(const GnArgs& a, int64_t n, int64_t c, GnAffine<V, ACCURATE>& f)
+template <int V>
+__device__ __forceinline__ void gn_affine(const GnArgs& a, int64_t n, int64_t c, GnAffine<V>& f)
 {
     gn_channels<V>(a, n, c, [&](int j, float mean, float rstd, int64_t) {
         f.set(j, mean, rstd, a.gamma ? a.gamma[c + j] : 1.f, a.beta ? a.beta[c + j] : 0.f);
     });
 }
-// dx = dz scale + centre(x) slope + offset, from the group's means of gamma dz and gamma dz xh.
-template <bool ACCURATE>
-__device__ __forceinline__ void gn_gradient_terms(float2 means, float mean, float rstd, float& slope, float& offset)
+// dx = dz scale + (x - mean) slope + offset, from the group's means of gamma dz and gamma dz xh.
+__device__ __forceinline__ void gn_gradient_terms(float2 means, float rstd, float& slope, float& offset)
 {
     slope = -__fmul_rn(__fmul_rn(rstd, rstd), means.y);
     offset = -__fmul_rn(rstd, means.x);
-    if constexpr (!ACCURATE) offset = __fmaf_rn(-mean, slope, offset);
 }
 // V elements as they lie in memory.
 template <class E, int V> struct GnRaw { E e; };

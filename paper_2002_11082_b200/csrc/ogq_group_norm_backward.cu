@@ -14,9 +14,9 @@ template <class E, int V, bool KEPT>
 struct GnPair {
     GnRaw<E, V> dy;
     std::conditional_t<KEPT, GnKept<V>, GnRaw<E, V>> x;
-    // dz, and x less the mean or as it is
-    template <int ACT, bool ACCURATE, bool CENTRED>
-    __device__ __forceinline__ void open(int act, const GnAffine<V, CENTRED>& f, float (&dz)[V], float (&xc)[V]) const
+    // dz, and x less the mean
+    template <int ACT, bool ACCURATE>
+    __device__ __forceinline__ void open(int act, const GnAffine<V>& f, float (&dz)[V], float (&xc)[V]) const
     {
         gn_open<E, V>(dy, dz);
         if constexpr (KEPT) gn_open<V>(x, xc);
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(E) == 4 ? 2 : 3) k_gn_grad_su
     const GnPlace q = gn_place<V>(a.t);
     if (q.active) {
         const GnReader<E, V, KEPT> in(a, q);
-        GnAffine<V, true> f;  // sums of dz (x - mean): less the mean first, so that nothing is lost when they cancel
+        GnAffine<V> f;  // sums of dz (x - mean): less the mean first, so that nothing is lost when they cancel
         gn_affine(a, q.n, q.c, f);
         float sb[V], sg[V];
 #pragma unroll
@@ -173,11 +173,11 @@ __global__ void __launch_bounds__(kThreads) k_gn_grad(const __grid_constant__ Gn
     const GnPlace q = gn_place<V>(a.t);
     if (!q.active) return;
     const GnReader<E, V, KEPT> in(a, q);
-    GnAffine<V, kAccurate> f;
+    GnAffine<V> f;
     gn_affine(a, q.n, q.c, f);
     float slope[V], offset[V];
-    gn_channels<V>(a, q.n, q.c, [&](int j, float mean, float rstd, int64_t at) {
-        gn_gradient_terms<kAccurate>(__ldcg(a.sums + at), mean, rstd, slope[j], offset[j]);
+    gn_channels<V>(a, q.n, q.c, [&](int j, float, float rstd, int64_t at) {
+        gn_gradient_terms(__ldcg(a.sums + at), rstd, slope[j], offset[j]);
     });
     E* out = (E*)a.out + q.row * a.t.C + q.c;
     gn_pixels<GnPair<E, V, KEPT>, sizeof(E) == 2 ? 2 : 1>(q.count, [&](int i, GnPair<E, V, KEPT>& r) { in.fetch(i, r); },
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 3 : 2) k_gn_backward(const 
             rx[u] = in[u] ? load_raw8((const E*)a.x + row * a.t.C + q.c) : zero_raw8<E>();
         }
     }
-    GnAffine<8, true> z;
+    GnAffine<8> z;
     if (q.active) gn_affine(a, q.n, q.c, z);
     float dz[U][8];
     float2 sum[8];
@@ -310,8 +310,8 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 3 : 2) k_gn_backward(const 
     if (q.active) {
         float slope[8], offset[8];
         const int64_t base = q.n * a.t.G + (int)(q.c - q.c0) / s.per;  // the slab's first group
-        gn_channels<8>(a, q.n, q.c, [&](int j, float mean, float rstd, int64_t at) {
-            gn_gradient_terms<true>(sh_group[at - base], mean, rstd, slope[j], offset[j]);
+        gn_channels<8>(a, q.n, q.c, [&](int j, float, float rstd, int64_t at) {
+            gn_gradient_terms(sh_group[at - base], rstd, slope[j], offset[j]);
         });
 #pragma unroll
         for (int u = 0; u < U; ++u) {

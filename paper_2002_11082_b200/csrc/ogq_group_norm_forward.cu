@@ -54,9 +54,11 @@ __global__ void __launch_bounds__(kThreads) k_gn_moments(const __grid_constant__
     for (int j = threadIdx.x; j < a.t.tx * V; j += kThreads) {
         const int64_t c = (int64_t)q.tile * a.t.tx * V + j;
         if (c >= a.t.C) break;
+        // about the first row's mean, which a chunk always has: the mean of one value everywhere is that value
+        const float first = sh[j].x;
         float sum = 0.f;
-        for (int y = 0; y < a.t.ty; ++y) sum = __fmaf_rn(y < more ? w1 : w0, whole || y < more ? sh[y * a.t.tx * V + j].x : 0.f, sum);
-        const float mean = __fmul_rn(sum, inv);
+        for (int y = 1; y < a.t.ty; ++y) sum = __fmaf_rn(y < more ? w1 : w0, whole || y < more ? __fsub_rn(sh[y * a.t.tx * V + j].x, first) : 0.f, sum);
+        const float mean = __fmaf_rn(sum, inv, first);
         float m2 = 0.f;
         for (int y = 0; y < a.t.ty; ++y) {
             const float2 e = sh[y * a.t.tx * V + j];
@@ -140,7 +142,7 @@ __global__ void __launch_bounds__(kThreads) k_gn_apply(const __grid_constant__ G
     constexpr bool kAccurate = sizeof(E) == 4;
     const GnPlace q = gn_place<V>(a.t);
     if (!q.active) return;  // KEEP: whole groups of lanes, since tx is a multiple of 4
-    GnAffine<V, kAccurate> f;
+    GnAffine<V> f;
     gn_affine(a, q.n, q.c, f);
     const unsigned team = 0xfu << (threadIdx.x & 28);
     const int64_t at = q.row * a.t.C + q.c;
@@ -167,15 +169,16 @@ __global__ void __launch_bounds__(kThreads) k_gn_apply(const __grid_constant__ G
                            });
 }
 
-// The whole pass of one slab (see ogq_group_norm_resident.cuh): x is read once.  The CTA's mean and its sum of squares about that
-// mean, then joined over the cluster.
+// The whole pass of one slab (see ogq_group_norm_resident.cuh): x is read once.  The CTA's mean, of plain sums; the sum of what deviates from it, which
+// corrects it, and of the squares; then joined over the cluster about the first CTA's mean.  (Plain sums of one value c need not give c: 0.04 off after rstd = 316 at 1000.)
 template <class E, int ACT, int KEEP, int U>
 __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_forward(const __grid_constant__ GnArgs a, const __grid_constant__ GnSlab s)
 {
     pdl_wait();
     pdl_launch_dependents();
     constexpr bool kAccurate = sizeof(E) == 4;
-    __shared__ float sh[kThreads * 8];
+    __shared__ float2 sh2[kThreads * 8];
+    float* sh = reinterpret_cast<float*>(sh2);
     __shared__ float sh_mean[kGnMaxWidth], sh_rstd[kGnMaxWidth];
     __shared__ float2 sh_cta[kGnMaxWidth];
     const GnSpot q = gn_spot(a.t, s);
@@ -213,6 +216,7 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_fo
     }
     __syncthreads();
     float m[8];
+    float2 dev[8];
     {
         int g = q.c0 / s.per, left = (g + 1) * s.per - q.c0;
 #pragma unroll
@@ -220,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_fo
             if (left == 0) { ++g; left = s.per; }
             --left;
             m[j] = sh_mean[g];
-            sum[j] = 0.f;
+            dev[j] = make_float2(0.f, 0.f);
         }
     }
 #pragma unroll
@@ -230,18 +234,30 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_fo
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float d = in[u] ? __fsub_rn(f[j], m[j]) : 0.f;
-            sum[j] = __fmaf_rn(d, d, sum[j]);
+            dev[j].x = __fadd_rn(dev[j].x, d);
+            dev[j].y = __fmaf_rn(d, d, dev[j].y);
         }
     }
-    gn_put_sums(s, q, sum, sh, s.width);
+    gn_put_sums(s, q, dev, sh2, s.width);
     __syncthreads();
     for (int g = warp; g < groups; g += kWarps) {
-        float t = 0.f;
+        float2 t = make_float2(0.f, 0.f);
         for (int c = lane; c < s.per; c += 32)
-            for (int r = 0; r < s.sum_rows; ++r) t += sh[r * s.width + g * s.per + c];
+            for (int r = 0; r < s.sum_rows; ++r) {
+                const float2 e = sh2[r * s.width + g * s.per + c];
+                t.x += e.x;
+                t.y += e.y;
+            }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-        if (lane == 0) sh_cta[g] = make_float2(sh_mean[g], t);
+        for (int o = 16; o > 0; o >>= 1) {
+            t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
+            t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
+        }
+        const float by = count > 0.f ? t.x / count : 0.f;
+        if (lane == 0) {
+            const float m2 = __fmaf_rn(-by, t.x, t.y);
+            sh_cta[g] = make_float2(sh_mean[g] + by, m2 < 0.f ? 0.f : m2);  // (a NaN stays one)
+        }
     }
     if (s.cluster > 1) {
         gn_cluster_arrive();
@@ -258,10 +274,11 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_fo
             n = last > first ? (float)((int)(last - first) * s.per) : 0.f;
         }
         const float all = (float)(a.t.P * s.per);
-        float mean = n > 0.f ? n * e.x : 0.f;
+        const float first = __shfl_sync(0xffffffffu, e.x, 0);
+        float mean = n > 0.f ? n * (e.x - first) : 0.f;
 #pragma unroll
         for (int o = kGnMaxCluster / 2; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
-        mean = __shfl_sync(0xffffffffu, mean, 0) / all;
+        mean = first + __shfl_sync(0xffffffffu, mean, 0) / all;
         const float d = e.x - mean;
         float m2 = n > 0.f ? __fmaf_rn(n * d, d, e.y) : 0.f;
 #pragma unroll
@@ -280,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_fo
     __syncthreads();
     if (s.cluster > 1) gn_cluster_arrive();  // this CTA has read the others' sums
     if (q.active) {
-        GnAffine<8, kAccurate> z;
+        GnAffine<8> z;
         int g = q.c0 / s.per, left = (g + 1) * s.per - q.c0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
