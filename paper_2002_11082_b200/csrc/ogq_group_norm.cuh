@@ -29,7 +29,7 @@ inline GnTiles gn_tiles(int64_t N, int64_t P, int64_t C, int64_t G, int V, int64
     t.cv = (int)(C / V);
     t.tx = t.cv < kThreads ? t.cv : kThreads;
     t.ty = kThreads / t.tx;
-    t.ctiles = (t.cv + t.tx - 1) / t.tx;
+    t.ctiles = (int)(((int64_t)t.cv + t.tx - 1) / t.tx);
     const int64_t units = (P + t.ty - 1) / t.ty, tasks = N * t.ctiles;  // pixels a thread of a sample, samples and tiles across
     int64_t px = kGnMaxPx;
     if (tasks > 0) {
@@ -133,9 +133,9 @@ __device__ __forceinline__ GnPlace gn_place(const GnTiles& t)
     q.ty = (int)(threadIdx.x / (uint32_t)t.tx);
     q.tx = (int)threadIdx.x - q.ty * t.tx;
     const int64_t first = (int64_t)q.chunk * (t.ty * t.px) + q.ty;
-    const int cv = q.tile * t.tx + q.tx;
+    const int64_t cv = (int64_t)q.tile * t.tx + q.tx;  // the last tile's may lie past 2^31
     q.active = q.ty < t.ty && cv < t.cv;
-    q.c = (int64_t)cv * V;
+    q.c = cv * V;
     q.row = q.n * t.P + first;
     const int64_t left = t.P - first;
     q.count = left <= 0 ? 0 : left >= (int64_t)t.ty * t.px ? t.px : min(t.px, (int)((uint32_t)(left - 1) / (uint32_t)t.ty) + 1);

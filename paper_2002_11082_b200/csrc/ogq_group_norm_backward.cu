@@ -391,10 +391,18 @@ cudaError_t launch_group_norm_backward(const GroupNorm& p, int sm_count, cudaStr
     cudaError_t e = launch(std::true_type{});
     if (e != cudaSuccess) return e;
     const int group_ctas = any ? (int)(p.N * p.G) : 0;
-    if (group_ctas + channel_ctas > 0) {
+    const auto join = [&](int groups, int channels) {
+        if (groups + channels == 0) return cudaSuccess;
         launch_begin("k_gn_grad_join", stream);
-        e = launch_pdl(k_gn_grad_join, group_ctas + channel_ctas, kThreads, 0, stream, a, group_ctas);
+        const cudaError_t r = launch_pdl(k_gn_grad_join, groups + channels, kThreads, 0, stream, a, groups);
         launch_end(stream);
+        return r;
+    };
+    if ((int64_t)group_ctas + channel_ctas <= 0x7fffffff) {
+        e = join(group_ctas, channel_ctas);
+    } else {  // more than a grid holds
+        e = join(group_ctas, 0);
+        if (e == cudaSuccess) e = join(0, channel_ctas);
     }
     if (e != cudaSuccess || !any) return e;
     return launch(std::false_type{});
