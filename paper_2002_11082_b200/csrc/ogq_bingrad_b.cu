@@ -94,6 +94,7 @@ __device__ __forceinline__ bool bb_advance(const PartSum& a, int pass, int lloyd
 // Barrier of the cluster's CTAs; shared-memory writes before it are seen after it.
 __device__ __forceinline__ void cluster_sync()
 {
+    __syncwarp();  // .aligned: the lanes of a warp must come together
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 

@@ -325,10 +325,7 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 3 : 2) k_gn_backward(const 
             store8((E*)a.out + row * a.t.C + q.c, f);
         }
     }
-    if (s.cluster > 1) {
-        __syncwarp();
-        gn_cluster_wait();  // the others have read this CTA's
-    }
+    if (s.cluster > 1) gn_cluster_wait();  // the others have read this CTA's
 }
 
 cudaError_t launch_group_norm_backward(const GroupNorm& p, int sm_count, cudaStream_t stream)

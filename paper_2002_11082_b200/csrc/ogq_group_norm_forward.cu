@@ -327,10 +327,7 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_fo
             if (in[u]) store8((E*)a.out + row * a.t.C + q.c, y);
         }
     }
-    if (s.cluster > 1) {
-        __syncwarp();
-        gn_cluster_wait();  // the others have read this CTA's
-    }
+    if (s.cluster > 1) gn_cluster_wait();  // the others have read this CTA's
 }
 
 size_t ws_bytes_group_norm(int64_t N, int64_t P, int64_t C, int64_t G)

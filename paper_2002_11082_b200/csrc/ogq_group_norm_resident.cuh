@@ -72,8 +72,17 @@ __device__ __forceinline__ uint32_t gn_rank()
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void gn_cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
-__device__ __forceinline__ void gn_cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+// (.aligned: the lanes of a warp must come together, wherever the code before has taken them)
+__device__ __forceinline__ void gn_cluster_arrive()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void gn_cluster_wait()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
 // The float2 at `p` of this CTA's shared memory, in CTA `rank` of the cluster.
 __device__ __forceinline__ float2 gn_remote(const float2* p, uint32_t rank)
 {

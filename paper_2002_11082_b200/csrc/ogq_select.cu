@@ -3144,6 +3144,7 @@ static_assert(sizeof(CellSelect) <= kIndexBytes, "fits the solver's shared memor
 
 __device__ __forceinline__ void cluster_sync_all()
 {
+    __syncwarp();  // .aligned: the lanes of a warp must come together
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t cluster_address(const void* p, int rank)

@@ -24,6 +24,7 @@ __device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank)
 }
 __device__ __forceinline__ void cluster_sync()
 {
+    __syncwarp();  // .aligned: the lanes of a warp must come together
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 

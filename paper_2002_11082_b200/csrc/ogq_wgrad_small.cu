@@ -120,7 +120,6 @@ __global__ void __launch_bounds__(kThreads) k_wgrad_small(const __grid_constant_
         }
         put_bias(s);
     }
-    __syncwarp();
     gn_cluster_arrive();
     gn_cluster_wait();  // the others have read this CTA's
 }

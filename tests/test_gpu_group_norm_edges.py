@@ -146,3 +146,22 @@ def test_gradient_of_gamma_over_many_chunks(dtype, N, P, C, G):
     xh = (xn - ref.wide(c.mean.numpy(), C)) * ref.wide(c.rstd.numpy(), C)
     for got, terms in ((dg, dn * xh), (db, dn)):
         assert_near(got.numpy()[0], terms.sum(axis=(0, 1)), 80 * U24 * np.abs(terms).sum(axis=(0, 1)), "dgamma, dbeta")
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("N,P,C,G", [(1, 900, 96, 3), (1, 2000, 64, 64), (2, 60, 480, 2), (1, 100, 200, 5), (4, 333, 72, 3), (1, 700, 40, 8)])
+def test_slabs_of_uneven_widths_over_clusters(dtype, N, P, C, G):
+    """Clusters of one to eight CTAs whose warps hold different numbers of groups, channels or rows when they come to the cluster's barriers."""
+    c = Call(N, P, C, G, dtype)
+    x, dy, gamma, beta = inputs(N, P, C, c.dt, N + P + C + 2)
+    gd, bd, g64, b64 = gamma.cuda(), beta.cuda(), gamma.double().numpy(), beta.double().numpy()
+    first = None
+    for _ in range(3):
+        y, fw = kernels(lambda: c.forward(x, gd, bd, ogq.OGQ_ACT_SILU, keep=C % 32 == 0))
+        check_forward(c, x, y, g64, b64, ref.SILU)
+        (dx, dg, db), bw = kernels(lambda: c.backward(dy, x, gd, bd, ogq.OGQ_ACT_SILU))
+        assert fw == ["k_gn_forward"] and bw[0] == "k_gn_backward"
+        check_backward(c, dy, x.double().numpy(), c.mean.numpy(), c.rstd.numpy(), g64, b64, ref.SILU, dx, dg, db)
+        got = [t.t.clone() for t in (y, dx, dg, db)]
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
