@@ -133,9 +133,9 @@ __device__ __forceinline__ GnPlace gn_place(const GnTiles& t)
     q.ty = (int)(threadIdx.x / (uint32_t)t.tx);
     q.tx = (int)threadIdx.x - q.ty * t.tx;
     const int64_t first = (int64_t)q.chunk * (t.ty * t.px) + q.ty;
-    const int64_t cv = (int64_t)q.tile * t.tx + q.tx;  // the last tile's may lie past 2^31
-    q.active = q.ty < t.ty && cv < t.cv;
-    q.c = cv * V;
+    const uint32_t cv = (uint32_t)q.tile * (uint32_t)t.tx + (uint32_t)q.tx;  // the last tile's may lie past 2^31
+    q.active = q.ty < t.ty && cv < (uint32_t)t.cv;
+    q.c = (int64_t)cv * V;
     q.row = q.n * t.P + first;
     const int64_t left = t.P - first;
     q.count = left <= 0 ? 0 : left >= (int64_t)t.ty * t.px ? t.px : min(t.px, (int)((uint32_t)(left - 1) / (uint32_t)t.ty) + 1);
