@@ -165,3 +165,30 @@ def test_slabs_of_uneven_widths_over_clusters(dtype, N, P, C, G):
         got = [t.t.clone() for t in (y, dx, dg, db)]
         first = first or got
         assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+@pytest.mark.parametrize("N,P,C,G", STREAMED + RESIDENT[2:3])
+def test_in_place_and_replayed(N, P, C, G):
+    """y over x and dx over dy, captured: every replay on fresh inputs gives the bits of the calls on buffers of their own."""
+    c = Call(N, P, C, G, "bf16")
+    x, dy, gamma, beta = inputs(N, P, C, c.dt, 31)
+    gd, bd = gamma.cuda(), beta.cuda()
+    y = c.forward(x, gd, bd, ogq.OGQ_ACT_SILU).t.clone()
+    codes, scales = c.codes.t.clone(), c.scales.t.clone()
+    want = [t.t.clone() for t in c.backward(dy, None, gd, bd, ogq.OGQ_ACT_SILU)]
+    a, b = x.cuda().view(N * P, C).clone(), dy.cuda().view(N * P, C).clone()
+    dg, db = torch.zeros(C, device="cuda"), torch.zeros(C, device="cuda")
+    size = (N, P, C, G, c.d)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ogq.ogq_group_norm_forward(a, *size, gd, bd, EPS, ogq.OGQ_ACT_SILU, 0, 0, 0, a, c.mean.t, c.rstd.t, c.codes.t, c.scales.t, c.ws, c.ws.numel())
+        ogq.ogq_group_norm_backward(b, None, c.codes.t, c.scales.t, *size, gd, bd, ogq.OGQ_ACT_SILU, c.mean.t, c.rstd.t, b, dg, db, c.ws, c.ws.numel())
+    for _ in range(3):
+        a.copy_(x.view(N * P, C))
+        b.copy_(dy.view(N * P, C))
+        c.codes.t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a, y) and torch.equal(c.codes.t, codes) and torch.equal(c.scales.t, scales)
+        assert torch.equal(b, want[0]) and torch.equal(dg, want[1][0]) and torch.equal(db, want[2][0])
+    del graph
