@@ -293,7 +293,7 @@ ogq_status ogq_bucket_decode_sum(const uint32_t *const *d_packed_k, const float 
  *
  * Types: `dtype` is the type of the activations and of their gradients, one of ogq_dtype.  Parameters, statistics and the
  * gradients of parameters are fp32 (the gradient of a weight can so be written straight into the gradient bucket).
- * Arithmetic is fp32 whatever the type; a result is rounded once, to nearest.
+ * Arithmetic is fp32 whatever the type (f below); a result is rounded once more, to nearest.
  *
  * Format of a matrix [rows, cols].  d_codes: int8 [rows, cols], contiguous.  d_scales: uint8 [rows, ogq_act8_groups(cols)],
  * contiguous; byte j of a row belongs to the row's columns 32 j ... 32 j + 31 (the last group may be shorter).
@@ -317,6 +317,10 @@ ogq_status ogq_bucket_decode_sum(const uint32_t *const *d_packed_k, const float 
  *   ogq_act8_backward: dx = dy f'(x^) [up^], dup = dy f(x^), from the kept x^ [and up^].  d_dup, d_up_codes and d_up_scales are all
  *     given or all NULL.
  * f is one of ogq_activation: the identity, ReLU (slope 0 at 0), x / (1 + exp(-x)), x Phi(x) with Phi the normal distribution function.
+ * Before the last rounding f(x) is off, as a share of itself, by at most (h = 2^-24): x / (1 + exp(-x)) in OGQ_F32 10 h, otherwise (10 + 2 |x|) h; x Phi(x) in OGQ_F32
+ * 1.2e-7 + (32 + 7 (x^2/2 + 1.3)) h, otherwise 1.7e-6 in place of the 1.2e-7; its slope by as much of the magnitudes of its two terms, or, that
+ * of x / (1 + exp(-x)) otherwise, by 10 (1 + |x|) h.  Where exp(-x^2/2) or
+ * 1 / (1 + exp(-x)) is below 2^-126 it counts as 0.
  */
 typedef enum { OGQ_F32 = 0, OGQ_F16 = 1, OGQ_BF16 = 2 } ogq_dtype;
 typedef enum { OGQ_ACT_NONE = 0, OGQ_ACT_RELU = 1, OGQ_ACT_SILU = 2, OGQ_ACT_GELU = 3 } ogq_activation;
@@ -342,8 +346,9 @@ ogq_status ogq_act8_backward(const void *d_dy, int64_t ld_dy, const int8_t *d_co
  *   dW[o][i] = sum_t dy[t][o] x^[t][i],   db[o] = sum_t dy[t][o],   t < rows, i < cols, o < out_cols.
  * d_dy [rows, out_cols] of type dtype with row stride ld_dy; d_dw fp32 [out_cols, cols], contiguous; d_db fp32 [out_cols] or NULL.
  * accumulate = 0: the outputs are overwritten; 1: the sums are added to what they hold.  rows = 0 gives sums of 0.
- * Products are exact and sums are fp32; the order of the additions depends on the sizes, the type, the alignment of the addresses and the
- * number of SMs only, so the same call gives the same bits again.  d_ws: scratch of ogq_act8_wgrad_workspace_bytes (a size for the current device), 256-byte aligned.
+ * Products are exact and sums are fp32 (few rows and weights: products and sums are fp32 multiply-adds, rounded together); which, and the order of the additions, depends
+ * on the sizes, the type, the alignment of the addresses and strides, whether d_db is given, and the number of SMs, on nothing else: the same call gives the same bits
+ * again, but a call without d_db may round dW differently.  d_ws: scratch of ogq_act8_wgrad_workspace_bytes (a size for the current device), 256-byte aligned.
  * Should a wait inside the kernel run out (four seconds), its part of the outputs is NaN.
  */
 size_t ogq_act8_wgrad_workspace_bytes(int64_t rows, int64_t cols, int64_t out_cols, int dtype);
@@ -363,7 +368,9 @@ ogq_status ogq_act8_wgrad(const void *d_dy, int64_t ld_dy, const int8_t *d_codes
  *             d_dgamma and d_dbeta fp32 [C], overwritten; each may be NULL.
  * The variance is taken about the mean (no difference of large sums).  N, P or C may be 0 (sums over nothing are 0, so is the mean).
  * G divides C, eps > 0.  P C/G, N G and N * ceil(C/32) * P are below 2^31 (OGQ_ERR_UNSUPPORTED).  The order of the additions
- * depends on the sizes and the number of SMs only.  d_ws: scratch of ogq_group_norm_workspace_bytes, 256-byte aligned.
+ * depends on the sizes, the type, the activation, the alignment of the addresses, whether codes are given, and the device, on nothing else: the same call gives the same bits
+ * again.  All kernels take x less the mean first, and both passes compute z = gamma_c xh + beta_c alike: from x itself they take the same side of ReLU.
+ * d_ws: scratch of ogq_group_norm_workspace_bytes, 256-byte aligned.
  * d_y may be d_x and d_dx may be d_dy; outputs overlap nothing else.
  */
 size_t ogq_group_norm_workspace_bytes(int64_t N, int64_t P, int64_t C, int64_t G);

@@ -1,7 +1,7 @@
 // Activations kept in 8 bits: the decoder, and the backward pass of the activation function from its kept inputs.
 //   dx = dy f'(x^) [up^],  dup = dy f(x^)
 // Bound by memory: dy and 33/32 bytes per kept element read once, the gradients written once.  16,384 x 4096 bf16 decoded: 33 us, 6.2 TB/s; gated
-// SiLU on 8192 x 8192 bf16: 84 us, 6.4 TB/s.  GELU in 16 bits is bound by its 36 instructions an element.
+// SiLU on 8192 x 8192 bf16: 84 us, 6.4 TB/s.  GELU in 16 bits is bound by its 37 instructions an element.
 #include "ogq_act8.cuh"
 #include "ogq_internal.h"
 

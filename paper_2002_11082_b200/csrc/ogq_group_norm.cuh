@@ -47,7 +47,7 @@ inline GnTiles gn_tiles(int64_t N, int64_t P, int64_t C, int64_t G, int V, int64
     return t;
 }
 
-// CTAs of a kernel that run at a time (looked up once per kernel).
+// CTAs of a kernel that run at a time, asked of the runtime at every launch (it depends on the instantiation and on the device).
 template <class K>
 inline int64_t gn_wave(K kernel, int sm_count)
 {

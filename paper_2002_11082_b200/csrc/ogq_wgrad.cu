@@ -11,7 +11,8 @@
 // nearest, while the next one grows in the other half of TMEM.
 //   Work is split by tile as long as there are tiles for all pairs; what is left (all of it, when weights are few and rows many) by
 // steps of 128 rows, partial tiles joined by a second kernel in a fixed order.
-//   What bounds it (16,384 x 4096 x 4096, 430 us, 1.28 PFLOP/s; the MMAs alone 281): shared memory, which 64 rows of a tile keep busy for 640
+//   What bounds it (16,384 x 4096 x 4096: this kernel alone in a short run 430 us, 1.28 PFLOP/s, the MMAs alone 281; the call with bias
+// and join 510, and 545 to 560 in steady use, where power takes the clocks down): shared memory, which 64 rows of a tile keep busy for 640
 // cycles (TMA writes 192, the converters read 64 and write 128, the MMAs read 256) where the MMAs take 512; in long runs, power.
 #include <cuda.h>
 
@@ -21,7 +22,8 @@
 
 namespace ogq {
 
-// Rows of t per stage: fewer barriers and commits a row than with 64 (16,384 x 4096 x 4096: 480 us, with 128 rows 437).
+// Rows of t per stage: fewer barriers and commits a row than with 64 (16,384 x 4096 x 4096, the product
+// alone in a short run: 480 us, with 128 rows 437).
 constexpr int kStepRows = 128;
 constexpr int kFlush = 4;                      // steps per running sum
 constexpr int kOperands = 2;                   // converted tiles of x^: one being written, one being multiplied
@@ -948,8 +950,8 @@ cudaError_t launch_act8_wgrad(const Wgrad8& p, int sm_count, cudaStream_t stream
     uint8_t* scales_to = (uint8_t*)kept + plan.kept_bytes;
 
     // One step of bf16 rows: the product's kernel adds up dy for the bias as well.  More: a kernel before it leaves sums over chunks of
-    // rows, which the product's kernel joins.  (All of it there, by the warp that TMA leaves free, took the product from 430 to 610 us at
-    // 16,384 x 4096 x 4096, against 30 us for the other kernel.)
+    // rows, which the product's kernel joins.  (All of it there, by the warp that TMA leaves free, took the product alone from 430 to 610 us at
+    // 16,384 x 4096 x 4096 in a short run, against 30 us for the other kernel.)
     const bool narrow = p.cols <= 128;
     const bool tma_scales = act8_groups(p.cols) % 16 == 0 && (lay_s || ((uintptr_t)p.scales & 15) == 0);
     const bool beside = p.db && p.cols > 0 && p.rows <= kBiasRows && p.dtype == OGQ_BF16;
