@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(kThreads) k_gn_moments(const __grid_constant__
                                    gn_open<E, V>(r, v);
                                    if (i == 0) {
 #pragma unroll
-                                       for (int j = 0; j < V; ++j) shift[j] = v[j];
+                                       for (int j = 0; j < V; ++j) shift[j] = fabsf(v[j]) < INFINITY ? v[j] : 0.f;
                                    }
 #pragma unroll
                                    for (int j = 0; j < V; ++j) {
@@ -58,7 +58,12 @@ __global__ void __launch_bounds__(kThreads) k_gn_moments(const __grid_constant__
         const float first = sh[j].x;
         float sum = 0.f;
         for (int y = 1; y < a.t.ty; ++y) sum = __fmaf_rn(y < more ? w1 : w0, whole || y < more ? __fsub_rn(sh[y * a.t.tx * V + j].x, first) : 0.f, sum);
-        const float mean = __fmaf_rn(sum, inv, first);
+        float mean = __fmaf_rn(sum, inv, first);
+        if (mean != mean) {  // infinities: of one sign, the mean is theirs
+            sum = 0.f;
+            for (int y = 0; y < a.t.ty; ++y) sum = __fmaf_rn(y < more ? w1 : w0, whole || y < more ? sh[y * a.t.tx * V + j].x : 0.f, sum);
+            mean = __fmul_rn(sum, inv);
+        }
         float m2 = 0.f;
         for (int y = 0; y < a.t.ty; ++y) {
             const float2 e = sh[y * a.t.tx * V + j];
@@ -256,7 +261,8 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_fo
         const float by = count > 0.f ? t.x / count : 0.f;
         if (lane == 0) {
             const float m2 = __fmaf_rn(-by, t.x, t.y);
-            sh_cta[g] = make_float2(sh_mean[g] + by, m2 < 0.f ? 0.f : m2);  // (a NaN stays one)
+            const float m = sh_mean[g];
+            sh_cta[g] = make_float2(fabsf(m) == INFINITY ? m : m + by, m2 < 0.f ? 0.f : m2);  // (a NaN stays one)
         }
     }
     if (s.cluster > 1) {
@@ -279,6 +285,12 @@ __global__ void __launch_bounds__(kThreads, U <= 2 ? 4 : U <= 4 ? 3 : 2) k_gn_fo
 #pragma unroll
         for (int o = kGnMaxCluster / 2; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
         mean = first + __shfl_sync(0xffffffffu, mean, 0) / all;
+        if (mean != mean) {  // infinities: of one sign, the mean is theirs (all lanes have the same value here)
+            mean = n > 0.f ? n * e.x : 0.f;
+#pragma unroll
+            for (int o = kGnMaxCluster / 2; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
+            mean = __shfl_sync(0xffffffffu, mean, 0) / all;
+        }
         const float d = e.x - mean;
         float m2 = n > 0.f ? __fmaf_rn(n * d, d, e.y) : 0.f;
 #pragma unroll

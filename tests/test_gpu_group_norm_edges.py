@@ -192,3 +192,29 @@ def test_in_place_and_replayed(N, P, C, G):
         assert torch.equal(a, y) and torch.equal(c.codes.t, codes) and torch.equal(c.scales.t, scales)
         assert torch.equal(b, want[0]) and torch.equal(dg, want[1][0]) and torch.equal(db, want[2][0])
     del graph
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("N,P,C,G", ALL)
+def test_mean_of_a_group_with_infinities(dtype, N, P, C, G):
+    """Infinities of one sign, at a thread's first pixel or a later one: the mean is that infinity, of both signs or with a NaN it is NaN; rstd is NaN and so are the
+    group's outputs.  The other groups are as without it, to the last bit."""
+    c = Call(N, P, C, G, dtype)
+    x, _, _, _ = inputs(N, P, C, c.dt, 33)
+    clean = [t.t.clone() for t in (c.forward(x, None, None, ogq.OGQ_ACT_NONE, keep=False), c.mean, c.rstd)]
+    inf = float("inf")
+    for at, value in ((((0, 0),), (inf,)), (((0, P - 1),), (-inf,)), (((0, 0), (0, P // 2), (0, P - 1)), (inf,) * 3), (((0, 1), (0, P - 1)), (inf, -inf)),
+                      (((0, P // 3),), (float("nan"),))):
+        z = x.clone()
+        for (n, p), v in zip(at, value):
+            z[n, p, C - 1] = v
+        y = c.forward(z, None, None, ogq.OGQ_ACT_NONE, keep=False)
+        want = sum(value)
+        got = float(c.mean.t[0, G - 1])
+        assert got == want or (got != got and want != want), (at, value, got)
+        assert bool(torch.isnan(c.rstd.t[0, G - 1])) and bool(torch.isnan(y.t.view(N, P, G, C // G)[0, :, G - 1]).all())
+        rest = torch.ones(N, G, dtype=torch.bool, device="cuda")
+        rest[0, G - 1] = False
+        assert torch.equal(c.mean.t[rest], clean[1][rest]) and torch.equal(c.rstd.t[rest], clean[2][rest])
+        pick = rest[:, None, :, None].expand(N, P, G, C // G)
+        assert torch.equal(y.t.view(N, P, G, C // G)[pick], clean[0].view(N, P, G, C // G)[pick])
